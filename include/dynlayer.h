@@ -461,6 +461,64 @@ dyn_status dyn_tune(dyn_layer *layer, const dyn_batch *batch, const int32_t *ctx
                     void *hip_stream, dyn_scheduler *s, dyn_schedule *out, dyn_tune_result *result,
                     dyn_tune_candidate *table, int capacity);
 
+/* ---- The care of a paged cache's pages ----------------------------------------------
+ *
+ * Between two steps a serving program grows sequences, forks one into several that go on from the same
+ * positions, cuts them back, frees them, and moves pages together.  These calls do that on the caller's pools: all
+ * layers' K and V pages in the layout of the header above, the block table, the cached positions of every
+ * row and the references to every page.  All of it is DEVICE memory, every decision is taken on the
+ * device, so the calls are asynchronous, allocate nothing, wait for nothing and may be captured into a graph; what a
+ * request came to is in its status word.  A pool that these calls keep obeys
+ *   ref_count[p] = number of (row r, j < ceil(seq_len[r] / page_size)) with block_table[r][j] = p, plus whatever
+ *                  references the caller counts on top for itself (a prefix it keeps); 0: the page is free;
+ *   a last page that is partly filled is named by one row only: what a row appends, no other row sees.
+ * Pages are taken in ascending order, by the requests in their order; a request is served if the pages that it and all
+ * before it ask for are there (refused ones ask for none).  Pages that a call gives up are free for the next call, not for its own
+ * requests.  The values of the arrays are read on the device: a page or row number outside the pool is never
+ * followed.  Calls that share a pool or a workspace must be ordered (one stream, or events). */
+typedef struct {
+    int dtype, n_layers, n_kv_heads, head_dim, page_size;
+    int n_pages;                       /* pages of each layer's pools */
+    int n_rows, max_pages_per_row;     /* rows of the block table, and their width */
+    void *k_cache, *v_cache;           /* layer 0; 16-byte aligned */
+    size_t kv_layer_stride;            /* bytes from layer l's cache to layer l+1's (both caches); a multiple of 16 */
+    void *const *k_cache_layers;       /* as in dyn_batch: HOST [n_layers] device pointers, or both NULL */
+    void *const *v_cache_layers;
+    int32_t *block_table;              /* [n_rows, max_pages_per_row]; a dyn_batch may use any run of its rows */
+    int32_t *seq_len;                  /* [n_rows] positions of each row; 0: the row is empty */
+    int32_t *ref_count;                /* [n_pages] */
+    void *workspace;                   /* >= dyn_pages_workspace_bytes(...), 256-byte aligned; not read before it is written */
+    size_t workspace_bytes;
+} dyn_page_pool;
+
+enum {
+    DYN_PAGES_DONE = 0,
+    DYN_PAGES_NONE_LEFT = 1,           /* the free pages did not reach: the row is as it was */
+    DYN_PAGES_REFUSED = 2              /* a row or length outside the pool, a row named by an earlier request of the call, a fork onto
+                                          a row that is not empty: the row is as it was */
+};
+
+/* Workspace of calls with up to max_requests requests (0: dyn_pages_compact); 0 if the pool's sizes are not valid. */
+size_t dyn_pages_workspace_bytes(const dyn_page_pool *pool, int max_requests);
+
+/* Copies page src[i] to page dst[i] (DEVICE [n]) in every layer, K and V.  Tables and counts stay.  The dst pages are
+ * distinct and none is a src page; a pair with a page outside the pool is left out.  Needs no table and no workspace. */
+dyn_status dyn_pages_copy(const dyn_page_pool *pool, int n, const int32_t *src, const int32_t *dst, void *hip_stream);
+
+/* Makes the empty row child[i] a sequence with parent[i]'s positions (DEVICE [n]; a parent may be named often, rows are read as
+ * they are before the call).  Full pages are shared; a partly filled last page is copied to a free one, in every layer.
+ * status: DEVICE [n], written. */
+dyn_status dyn_pages_fork(const dyn_page_pool *pool, int n, const int32_t *parent, const int32_t *child, int32_t *status, void *hip_stream);
+
+/* Gives row[i] length[i] positions: it grows by free pages (their contents are whatever they held), or gives up the pages behind its
+ * new end (0: all of them).  A row cut back into a page that others name too gets a copy of it.  status as above. */
+dyn_status dyn_pages_resize(const dyn_page_pool *pool, int n, const int32_t *row, const int32_t *length, int32_t *status, void *hip_stream);
+
+/* Moves the pages that are not free to the front: n_live[0] (DEVICE) of them, and every one from there on takes
+ * the place of a free one below, the lowest the lowest, in every layer.  Block table and counts follow; new_page (DEVICE [n_pages],
+ * written) says where each page is now, -1 for one that was free. */
+dyn_status dyn_pages_compact(const dyn_page_pool *pool, int32_t *new_page, int32_t *n_live, void *hip_stream);
+
 /* ---- Measurement aid -----------------------------------------------------------------
  *
  * The layer's dominant operators are bound by HBM bandwidth (the memory-bound operator class

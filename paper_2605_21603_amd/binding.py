@@ -105,12 +105,22 @@ class dyn_slot_time(C.Structure):
                 ("stop_ms", C.c_float)]
 
 
+class dyn_page_pool(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("dtype", "n_layers", "n_kv_heads", "head_dim", "page_size", "n_pages", "n_rows", "max_pages_per_row")] + \
+               [("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("kv_layer_stride", C.c_size_t), ("k_cache_layers", C.c_void_p),
+                ("v_cache_layers", C.c_void_p), ("block_table", C.c_void_p), ("seq_len", C.c_void_p), ("ref_count", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+DYN_PAGES_DONE, DYN_PAGES_NONE_LEFT, DYN_PAGES_REFUSED = 0, 1, 2
+
 EXPORTS = ["dyn_layer_create", "dyn_layer_destroy", "dyn_layer_workspace_bytes", "dyn_schedule_validate",
            "dyn_layer_prepare", "dyn_layer_release_graphs", "dyn_layer_forward", "dyn_layer_forward_noalloc", "dyn_layer_set_profiling", "dyn_layer_get_slot_times", "dyn_last_error",
            "dyn_scheduler_create", "dyn_scheduler_destroy", "dyn_scheduler_split", "dyn_scheduler_set_partitions",
            "dyn_scheduler_get_ready_ops", "dyn_scheduler_execute", "dyn_scheduler_finish", "dyn_policy_auto",
            "dyn_tune_candidates", "dyn_tune_record", "dyn_tune", "dyn_schedule_memory", "dyn_schedule_workspace_bytes",
-           "dyn_schedule_regions", "dyn_probe_hbm_read", "dyn_probe_mfma_loop"]
+           "dyn_schedule_regions", "dyn_probe_hbm_read", "dyn_probe_mfma_loop",
+           "dyn_pages_workspace_bytes", "dyn_pages_copy", "dyn_pages_fork", "dyn_pages_resize", "dyn_pages_compact"]
 
 _lib = None
 
@@ -154,6 +164,12 @@ def lib() -> C.CDLL:
         l.dyn_tune_record.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p]
         l.dyn_tune.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                C.c_void_p, C.c_void_p, C.c_int]
+        l.dyn_pages_workspace_bytes.restype = C.c_size_t
+        l.dyn_pages_workspace_bytes.argtypes = [C.c_void_p, C.c_int]
+        l.dyn_pages_copy.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+        l.dyn_pages_fork.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        l.dyn_pages_resize.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        l.dyn_pages_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         _lib = l
     return _lib
 
@@ -523,3 +539,82 @@ class DeviceStep:
         # uploads were queued on torch's current stream; forwards run on other, non-blocking
         # streams, so wait here until the inputs have landed
         torch.cuda.synchronize(dev)
+
+
+def _stream_of(stream: Optional[torch.cuda.Stream], device) -> C.c_void_p:
+    return C.c_void_p((stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream)
+
+
+def _int32(t: torch.Tensor, name: str, device, shape) -> int:
+    """Device pointer of a contiguous int32 tensor of that shape on that device."""
+    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s: a contiguous int32 tensor of shape %s on %s, not %s %s on %s" %
+                         (name, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+class PagePool:
+    """A paged cache and the tables that say what its pages hold (dyn_page_pool), with the calls that keep both.
+
+    k_cache [layers, pages, kv heads, page size, head dim] and v_cache [layers, pages, kv heads, head dim, page size], or lists of
+    one tensor per layer; block_table [rows, pages per row], seq_len [rows] and ref_count [pages] int32, all on one device.
+    The calls run on `stream` (default: torch's current one on that device), change the tensors in place and wait for
+    nothing.  max_requests: the most requests a fork or resize will have; the workspace is sized for it."""
+
+    def __init__(self, k_cache, v_cache, block_table: torch.Tensor, seq_len: torch.Tensor, ref_count: torch.Tensor, max_requests: int):
+        ks, vs = list(k_cache), list(v_cache)
+        k, v = ks[0], vs[0]
+        n_pages, n_kv, ps, hd = k.shape
+        self.device = k.device
+        for t, shape in [(t, (n_pages, n_kv, ps, hd)) for t in ks] + [(t, (n_pages, n_kv, hd, ps)) for t in vs]:
+            if tuple(t.shape) != shape or t.dtype != k.dtype or t.device != self.device or not t.is_contiguous():
+                raise ValueError("cache layer: a contiguous %s tensor of shape %s on %s" % (k.dtype, shape, self.device))
+        if len(ks) != len(vs) or k.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("as many K as V layers, float32 or bfloat16")
+        self.k_cache, self.v_cache, self.block_table, self.seq_len, self.ref_count = k_cache, v_cache, block_table, seq_len, ref_count
+        self.max_requests = int(max_requests)
+        rows, width = block_table.shape
+        self._ptrs = [(C.c_void_p * len(a))(*[t.data_ptr() for t in a]) for a in (ks, vs)]
+        self.pool = dyn_page_pool(DYN_F32 if k.dtype == torch.float32 else DYN_BF16, len(ks), n_kv, hd, ps, n_pages, rows, width, None, None, 0,
+                                  C.cast(self._ptrs[0], C.c_void_p), C.cast(self._ptrs[1], C.c_void_p),
+                                  _int32(block_table, "block_table", self.device, (rows, width)), _int32(seq_len, "seq_len", self.device, (rows,)),
+                                  _int32(ref_count, "ref_count", self.device, (n_pages,)), None, 0)
+        nbytes = lib().dyn_pages_workspace_bytes(C.byref(self.pool), self.max_requests)
+        if nbytes == 0:
+            raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error() or "max_requests = %d" % self.max_requests)
+        self._workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        self.pool.workspace = (self._workspace.data_ptr() + 255) & ~255
+        self.pool.workspace_bytes = nbytes
+
+    def copy(self, src: torch.Tensor, dst: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Pages src[i] to dst[i], in every layer."""
+        n = len(src)
+        _check(lib().dyn_pages_copy(C.byref(self.pool), n, _int32(src, "src", self.device, (n,)), _int32(dst, "dst", self.device, (n,)),
+                                    _stream_of(stream, self.device)))
+
+    def _requests(self, call, a, b, names, status, stream) -> torch.Tensor:
+        n = len(a)
+        if status is None:
+            status = torch.empty(n, dtype=torch.int32, device=self.device)
+        _check(call(C.byref(self.pool), n, _int32(a, names[0], self.device, (n,)), _int32(b, names[1], self.device, (n,)),
+                    _int32(status, "status", self.device, (n,)), _stream_of(stream, self.device)))
+        return status
+
+    def fork(self, parent: torch.Tensor, child: torch.Tensor, status: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Row child[i] goes on from row parent[i]'s positions; returns the DYN_PAGES_* status words."""
+        return self._requests(lib().dyn_pages_fork, parent, child, ("parent", "child"), status, stream)
+
+    def resize(self, row: torch.Tensor, length: torch.Tensor, status: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Row row[i] has length[i] positions from now on (0: freed); returns the DYN_PAGES_* status words."""
+        return self._requests(lib().dyn_pages_resize, row, length, ("row", "length"), status, stream)
+
+    def compact(self, new_page: Optional[torch.Tensor] = None, n_live: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """Moves the pages in use to the front; returns (where each page is now, -1 if it was free; how many are in use)."""
+        n = self.pool.n_pages
+        new_page = torch.empty(n, dtype=torch.int32, device=self.device) if new_page is None else new_page
+        n_live = torch.empty(1, dtype=torch.int32, device=self.device) if n_live is None else n_live
+        _check(lib().dyn_pages_compact(C.byref(self.pool), _int32(new_page, "new_page", self.device, (n,)), _int32(n_live, "n_live", self.device, (1,)),
+                                       _stream_of(stream, self.device)))
+        return new_page, n_live
