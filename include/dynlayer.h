@@ -114,6 +114,9 @@ typedef struct {
                                       layer's K and V pool can be placed on its own.  Where the two pools of a layer lie
                                       in HBM changes the rate of the attention launch that reads them together by up to
                                       14 % on MI355X (measured; see dyn_layer_forward) */
+    const int32_t *prefix_lead;    /* [n_seqs] each, or both NULL: sequences that begin with the same pages (see */
+    const int32_t *prefix_pages;   /* dyn_attn_shared).  The attention reads those pages once for all of them; y and the caches are what
+                                      they are without, to rounding.  The step's own tokens stand behind the shared pages */
 } dyn_batch;
 
 /* One dispatch: operator `op` over micro-batches nano .. nano + n_nano - 1 (n_nano = 1 is
@@ -159,7 +162,8 @@ void dyn_layer_destroy(dyn_layer *layer);
 /* Bytes of workspace that suffice for ANY legal schedule of a forward of up to max_tokens
  * tokens when no sequence has more than max_pages_per_seq pages: every intermediate and every
  * operator's scratch for the whole batch at once, nothing shared.  A particular schedule
- * usually needs much less: see dyn_schedule_workspace_bytes. */
+ * usually needs much less: see dyn_schedule_workspace_bytes.  For batches without prefix_lead; with it the same bound is
+ * dyn_memory_report.workspace_bytes. */
 size_t dyn_layer_workspace_bytes(const dyn_layer *layer, int max_tokens, int max_pages_per_seq);
 
 /* Host-only check of a schedule against a batch's shapes (no device memory is read):
@@ -460,6 +464,45 @@ dyn_status dyn_tune_record(dyn_scheduler *s, const dyn_tune_candidate *c, int n_
 dyn_status dyn_tune(dyn_layer *layer, const dyn_batch *batch, const int32_t *ctx_len_host, const dyn_tune_options *opt,
                     void *hip_stream, dyn_scheduler *s, dyn_schedule *out, dyn_tune_result *result,
                     dyn_tune_candidate *table, int capacity);
+
+/* ---- Attention over shared prefixes --------------------------------------------------
+ *
+ * Causal paged attention of n_tokens query rows, outside a layer: row t is a token of sequence seq_of_token[t] at position
+ * pos_of_token[t] and attends the cached keys 0 .. pos of that sequence (all of them are in the cache: nothing is appended, nothing
+ * rotated), scaled by 1 / sqrt(head_dim).  A row of position -1 attends nothing and its output is zero.
+ * prefix_lead[s] and prefix_pages[s] say what sequences have in common: the first prefix_pages[s] pages of row s of the block
+ * table are those of row prefix_lead[s], and every sequence with that lead and that many pages shares them (a sequence
+ * that shares nothing: 0 pages).  Shared pages are read once, through the lead's row, for all rows of adjacent tokens whose sequences
+ * share them, in one matrix product; the keys behind them are attended by each sequence for itself, and the two parts are
+ * merged.  It is a promise about the tables, not another attention: the result is that of every row over its own sequence,
+ * up to rounding.  Where it cannot pay or hold - a lead that one sequence names, a token that stands inside the shared pages, a lead or page
+ * count outside the table, a batch of more than 8192 sequences, shapes whose attention does not run on the matrix cores (page_size no
+ * multiple of 16, head_dim below 32, more than 16 q heads per kv head) - keys are attended without sharing.  A row's bits depend on its own
+ * sequence and on how many sequences of the batch name its lead.
+ * Tokens of one sequence are adjacent rows in position order. */
+typedef struct {
+    int dtype, n_q_heads, n_kv_heads, head_dim, page_size;
+    int kv_chunk_positions;            /* as in dyn_layer_config */
+    int n_tokens, n_seqs;
+    const void *q;                     /* [n_tokens, n_q_heads, head_dim], rows ld_q elements apart; 16-byte aligned rows */
+    int ld_q;
+    void *out;                         /* the same shape, rows ld_out elements apart, written; 16-byte aligned rows; not q */
+    int ld_out;
+    const int32_t *seq_of_token, *pos_of_token;     /* [n_tokens] */
+    const int32_t *block_table;        /* [n_seqs, max_pages_per_seq] */
+    int max_pages_per_seq;
+    const int32_t *prefix_lead, *prefix_pages;      /* [n_seqs], or both NULL */
+    const void *k_cache, *v_cache;     /* one layer's pools, 16-byte aligned */
+    void *workspace;                   /* >= dyn_attn_shared_workspace_bytes(...), 256-byte aligned; not read before it is written */
+    size_t workspace_bytes;
+} dyn_attn_batch;
+
+/* Workspace of a batch of these sizes (pointers are not looked at); 0 if they are not valid. */
+size_t dyn_attn_shared_workspace_bytes(const dyn_attn_batch *batch);
+
+/* Asynchronous on hip_stream; allocates nothing and may be captured into a graph (arrays may hold other values at every replay).
+ * Calls that overlap in time need workspaces of their own. */
+dyn_status dyn_attn_shared(const dyn_attn_batch *batch, void *hip_stream);
 
 /* ---- The care of a paged cache's pages ----------------------------------------------
  *

@@ -45,7 +45,8 @@ class dyn_batch(C.Structure):
                 ("seq_of_token", C.c_void_p), ("pos_of_token", C.c_void_p), ("block_table", C.c_void_p),
                 ("max_pages_per_seq", C.c_int), ("q_start_host", C.c_void_p), ("k_cache", C.c_void_p),
                 ("v_cache", C.c_void_p), ("kv_layer_stride", C.c_size_t), ("workspace", C.c_void_p),
-                ("workspace_bytes", C.c_size_t), ("k_cache_layers", C.c_void_p), ("v_cache_layers", C.c_void_p)]
+                ("workspace_bytes", C.c_size_t), ("k_cache_layers", C.c_void_p), ("v_cache_layers", C.c_void_p),
+                ("prefix_lead", C.c_void_p), ("prefix_pages", C.c_void_p)]
 
 
 class dyn_slot(C.Structure):
@@ -105,6 +106,14 @@ class dyn_slot_time(C.Structure):
                 ("stop_ms", C.c_float)]
 
 
+class dyn_attn_batch(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "kv_chunk_positions", "n_tokens", "n_seqs")] + \
+               [("q", C.c_void_p), ("ld_q", C.c_int), ("out", C.c_void_p), ("ld_out", C.c_int), ("seq_of_token", C.c_void_p),
+                ("pos_of_token", C.c_void_p), ("block_table", C.c_void_p), ("max_pages_per_seq", C.c_int), ("prefix_lead", C.c_void_p),
+                ("prefix_pages", C.c_void_p), ("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
 class dyn_page_pool(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("dtype", "n_layers", "n_kv_heads", "head_dim", "page_size", "n_pages", "n_rows", "max_pages_per_row")] + \
                [("k_cache", C.c_void_p), ("v_cache", C.c_void_p), ("kv_layer_stride", C.c_size_t), ("k_cache_layers", C.c_void_p),
@@ -120,7 +129,7 @@ EXPORTS = ["dyn_layer_create", "dyn_layer_destroy", "dyn_layer_workspace_bytes",
            "dyn_scheduler_get_ready_ops", "dyn_scheduler_execute", "dyn_scheduler_finish", "dyn_policy_auto",
            "dyn_tune_candidates", "dyn_tune_record", "dyn_tune", "dyn_schedule_memory", "dyn_schedule_workspace_bytes",
            "dyn_schedule_regions", "dyn_probe_hbm_read", "dyn_probe_mfma_loop",
-           "dyn_pages_workspace_bytes", "dyn_pages_copy", "dyn_pages_fork", "dyn_pages_resize", "dyn_pages_compact"]
+           "dyn_attn_shared_workspace_bytes", "dyn_attn_shared", "dyn_pages_workspace_bytes", "dyn_pages_copy", "dyn_pages_fork", "dyn_pages_resize", "dyn_pages_compact"]
 
 _lib = None
 
@@ -164,6 +173,9 @@ def lib() -> C.CDLL:
         l.dyn_tune_record.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p]
         l.dyn_tune.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                C.c_void_p, C.c_void_p, C.c_int]
+        l.dyn_attn_shared_workspace_bytes.restype = C.c_size_t
+        l.dyn_attn_shared_workspace_bytes.argtypes = [C.c_void_p]
+        l.dyn_attn_shared.argtypes = [C.c_void_p, C.c_void_p]
         l.dyn_pages_workspace_bytes.restype = C.c_size_t
         l.dyn_pages_workspace_bytes.argtypes = [C.c_void_p, C.c_int]
         l.dyn_pages_copy.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
@@ -494,8 +506,8 @@ class DeviceStep:
     caller has placed them layer by layer."""
 
     def __init__(self, layer: DynLayer, data: dict, device="cuda:0", sched: Optional["Schedule"] = None, guard: int = 0,
-                 placed: bool = False, workspace: Optional[torch.Tensor] = None):
-        """sched: size the workspace for this schedule alone (dyn_schedule_workspace_bytes) instead of
+                 placed: bool = False, workspace: Optional[torch.Tensor] = None, prefix: Optional[Sequence] = None):
+        """prefix: (prefix_lead, prefix_pages) per sequence, for sequences that begin with the same pages; sched: size the workspace for this schedule alone (dyn_schedule_workspace_bytes) instead of
         for any schedule; guard: extra bytes behind the workspace that the library is not told about;
         placed: data["k_cache"] / data["v_cache"] are lists of per-layer device tensors that stay
         where they are (k_cache_layers / v_cache_layers of the batch) instead of being stacked;
@@ -521,12 +533,21 @@ class DeviceStep:
         self.batch = dyn_batch(n_tokens, n_seqs, _ptr(self.x), _ptr(self.y), _ptr(self.seq_of_token),
                                _ptr(self.pos_of_token), _ptr(self.block_table), max_pages, _ptr(self.q_start_host),
                                _ptr(self.k_cache), _ptr(self.v_cache), stride, None, 0)
+        if prefix is not None:
+            self.prefix_lead, self.prefix_pages = (torch.as_tensor(np.ascontiguousarray(a, dtype=np.int32)).to(dev) for a in prefix)
+            assert len(self.prefix_lead) == len(self.prefix_pages) == n_seqs
+            self.batch.prefix_lead, self.batch.prefix_pages = self.prefix_lead.data_ptr(), self.prefix_pages.data_ptr()
         if placed:
             self._k_ptrs = (C.c_void_p * len(self.k_layers))(*[t.data_ptr() for t in self.k_layers])
             self._v_ptrs = (C.c_void_p * len(self.v_layers))(*[t.data_ptr() for t in self.v_layers])
             self.batch.k_cache_layers = C.cast(self._k_ptrs, C.c_void_p)
             self.batch.v_cache_layers = C.cast(self._v_ptrs, C.c_void_p)
-        nbytes = layer.workspace_bytes(n_tokens, max_pages) if sched is None else layer.schedule_workspace_bytes(self.batch, sched)
+        if sched is not None:
+            nbytes = layer.schedule_workspace_bytes(self.batch, sched)
+        elif prefix is not None:
+            nbytes = layer.memory(self.batch, sequential())["workspace_bytes"]
+        else:
+            nbytes = layer.workspace_bytes(n_tokens, max_pages)
         if workspace is not None:
             assert workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.numel() >= nbytes + 256 + guard
             self.workspace = workspace
@@ -553,6 +574,62 @@ def _int32(t: torch.Tensor, name: str, device, shape) -> int:
     return t.data_ptr()
 
 
+def _cache_pair(k: torch.Tensor, v: torch.Tensor):
+    """(pages, kv heads, page size, head dim) of one layer's K and V pool."""
+    if k.dim() != 4 or k.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("k_cache: float32 or bfloat16 of shape [pages, kv heads, page size, head dim], not %s %s" % (k.dtype, tuple(k.shape)))
+    n_pages, n_kv, ps, hd = k.shape
+    for t, shape in ((k, (n_pages, n_kv, ps, hd)), (v, (n_pages, n_kv, hd, ps))):
+        if tuple(t.shape) != shape or t.dtype != k.dtype or t.device != k.device or not t.is_contiguous():
+            raise ValueError("cache layer: a contiguous %s tensor of shape %s on %s, not %s %s" % (k.dtype, shape, k.device, t.dtype, tuple(t.shape)))
+    return n_pages, n_kv, ps, hd
+
+
+class SharedAttention:
+    """Attention of a batch whose sequences may share prefixes (dyn_attn_shared), on tensors that stay where they are.
+
+    q and out [tokens, q heads, head dim] with rows of any 16-byte aligned pitch; k_cache [pages, kv heads, page size, head dim] and
+    v_cache [pages, kv heads, head dim, page size] of one layer; seq_of_token, pos_of_token [tokens] (position -1: a
+    row that attends nothing), block_table [sequences, pages per sequence], prefix_lead and prefix_pages [sequences] int32.  All on
+    one device; their values may change between calls.  workspace: a device byte tensor to use instead of one of its own."""
+
+    def __init__(self, q: torch.Tensor, out: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, seq_of_token: torch.Tensor,
+                 pos_of_token: torch.Tensor, block_table: torch.Tensor, prefix_lead: Optional[torch.Tensor] = None,
+                 prefix_pages: Optional[torch.Tensor] = None, kv_chunk_positions: int = 0, workspace: Optional[torch.Tensor] = None):
+        _, n_kv, ps, hd = _cache_pair(k_cache, v_cache)
+        self.device = k_cache.device
+        T, n_q, _ = q.shape
+        for name, t in (("q", q), ("out", out)):
+            rows_ok = T <= 1 or t.stride(0) >= n_q * hd
+            if tuple(t.shape) != (T, n_q, hd) or t.dtype != k_cache.dtype or t.device != self.device or (T and t.stride()[1:] != (hd, 1)) or not rows_ok:
+                raise ValueError("%s: %s rows of [%d, %d] on %s, not %s %s of strides %s" % (name, k_cache.dtype, n_q, hd, self.device, t.dtype, tuple(t.shape), t.stride()))
+        if (prefix_lead is None) != (prefix_pages is None):
+            raise ValueError("prefix_lead and prefix_pages go together")
+        n_seqs, width = block_table.shape
+        pitch = lambda t: t.stride(0) if T > 1 else n_q * hd
+        ints = lambda t, name, n: _int32(t, name, self.device, (n,)) if t is not None else None
+        self._keep = (q, out, k_cache, v_cache, seq_of_token, pos_of_token, block_table, prefix_lead, prefix_pages)
+        self.out = out
+        self.batch = dyn_attn_batch(DYN_F32 if q.dtype == torch.float32 else DYN_BF16, n_q, n_kv, hd, ps, int(kv_chunk_positions), T, n_seqs,
+                                    q.data_ptr(), pitch(q), out.data_ptr(), pitch(out), ints(seq_of_token, "seq_of_token", T),
+                                    ints(pos_of_token, "pos_of_token", T), _int32(block_table, "block_table", self.device, (n_seqs, width)), width,
+                                    ints(prefix_lead, "prefix_lead", n_seqs), ints(prefix_pages, "prefix_pages", n_seqs),
+                                    k_cache.data_ptr(), v_cache.data_ptr(), None, 0)
+        nbytes = lib().dyn_attn_shared_workspace_bytes(C.byref(self.batch))
+        if nbytes == 0 and T:
+            raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error())
+        if workspace is not None and (workspace.dtype != torch.uint8 or workspace.device != self.device or workspace.numel() < nbytes + 256):
+            raise ValueError("workspace: %d bytes on %s" % (nbytes + 256, self.device))
+        self.workspace = workspace if workspace is not None else torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        self.batch.workspace = (self.workspace.data_ptr() + 255) & ~255
+        self.batch.workspace_bytes = nbytes
+
+    def forward(self, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Writes and returns `out`; on `stream`, by default torch's current one."""
+        _check(lib().dyn_attn_shared(C.byref(self.batch), _stream_of(stream, self.device)))
+        return self.out
+
+
 class PagePool:
     """A paged cache and the tables that say what its pages hold (dyn_page_pool), with the calls that keep both.
 
@@ -563,14 +640,11 @@ class PagePool:
 
     def __init__(self, k_cache, v_cache, block_table: torch.Tensor, seq_len: torch.Tensor, ref_count: torch.Tensor, max_requests: int):
         ks, vs = list(k_cache), list(v_cache)
-        k, v = ks[0], vs[0]
-        n_pages, n_kv, ps, hd = k.shape
+        if not ks or len(ks) != len(vs) or any(t.shape != ks[0].shape or t.dtype != ks[0].dtype or t.device != ks[0].device for t in ks):
+            raise ValueError("as many K as V layers, of one shape, type and device")
+        k = ks[0]
+        n_pages, n_kv, ps, hd = [_cache_pair(*pair) for pair in zip(ks, vs)][0]
         self.device = k.device
-        for t, shape in [(t, (n_pages, n_kv, ps, hd)) for t in ks] + [(t, (n_pages, n_kv, hd, ps)) for t in vs]:
-            if tuple(t.shape) != shape or t.dtype != k.dtype or t.device != self.device or not t.is_contiguous():
-                raise ValueError("cache layer: a contiguous %s tensor of shape %s on %s" % (k.dtype, shape, self.device))
-        if len(ks) != len(vs) or k.dtype not in (torch.float32, torch.bfloat16):
-            raise ValueError("as many K as V layers, float32 or bfloat16")
         self.k_cache, self.v_cache, self.block_table, self.seq_len, self.ref_count = k_cache, v_cache, block_table, seq_len, ref_count
         self.max_requests = int(max_requests)
         rows, width = block_table.shape

@@ -64,6 +64,9 @@ __device__ __forceinline__ void wait_vm(int n) {   // s_waitcnt vmcnt(n) only
 }
 
 // The items of the multi-token list, claimed until none is left, by a workgroup of kWaves * 64 threads with lds_bytes() of dynamic LDS.
+// PARTS: every item leaves partials for a merge of its own (kernels_attn_shared.hip), also where its chunk is all of what it was given.
+// ld_q: elements from a token's q heads to the next's; 0: rows of the fused projection, k and v heads behind them.
+template <bool PARTS = false>
 __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qkv,
                                                               const int32_t *__restrict__ seq_of_token,
                                                               const int32_t *__restrict__ pos_of_token,
@@ -73,7 +76,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                                                               bf16_t *__restrict__ out, int ld_out,
                                                               float *__restrict__ part_o, float *__restrict__ part_ml,
                                                               AttnShape sh, const int32_t *__restrict__ plan, int32_t *__restrict__ counter,
-                                                              const int32_t *__restrict__ ct_of_token) {
+                                                              const int32_t *__restrict__ ct_of_token, int ld_q = 0) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int32_t *pid = reinterpret_cast<int32_t *>(lds + kRing * kTile);      // physical pages of the chunk
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -84,7 +87,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
     const int wave_tok0 = wave * kSets * TG;                             // first token of the block this wave owns
     const float sscale = 1.4426950408889634f / sqrtf((float)HD);
     const int n_items = plan[0] * sh.n_kv;
-    const size_t row_elems = (size_t)(sh.n_q + 2 * sh.n_kv) * HD;
+    const size_t row_elems = PARTS && ld_q ? (size_t)ld_q : (size_t)(sh.n_q + 2 * sh.n_kv) * HD;
 
     // Work items are claimed from a counter in the list's header (zeroed by the work-list kernel),
     // longest first: the list is in token order, a block's keys grow with its position, so it is
@@ -377,7 +380,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
         for (int q = 0; q < kSets; ++q) {
             const ColumnEnd end = column_end(nk[q], lp0 * PS, chunk_pages * PS);
             if (end == COLUMN_NOT_MINE) continue;
-            if (end == COLUMN_DONE) {
+            if (!PARTS && end == COLUMN_DONE) {
                 const float inv = 1.0f / acc_l[q][0];
                 bf16_t *y = out + (size_t)(t0 + wave_tok0 + q * TG + col_tok) * ld_out + (g * G + col_head) * HD + 4 * lq;
 #pragma unroll

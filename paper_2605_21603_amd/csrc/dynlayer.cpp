@@ -21,6 +21,7 @@
 #include <string>
 #include <vector>
 
+#include "attn_shared.h"
 #include "kernels.h"
 
 namespace dyn {
@@ -81,7 +82,8 @@ struct WsLayout {
     size_t h, qkv, attn, x2, gu, act, xa, xb, plan, total;
     size_t sel, wgt;             // MoE routing: selected experts and their weights per token
     int ld_h, ld_attn, ld_act;   // padded row strides (elements) of the buffers the projections read
-    int max_chunks;
+    int max_chunks, prefix_chunks;
+    size_t plan_row;             // words of `plan` per token row
     std::vector<SlotScratch> slot;
 };
 
@@ -133,10 +135,12 @@ int qkv_width(const dyn_layer_config &c) { return (c.n_q_heads + 2 * c.n_kv_head
 struct Sizes {                  // bytes of each whole-batch tensor, and the row strides
     size_t h, qkv, attn, x2, gu, act, xa, xb, plan, sel, wgt;
     int ld_h, ld_attn, ld_act, max_chunks;
+    int prefix_chunks;          // of keys that sequences share, on top of max_chunks
+    size_t plan_row;            // words of the attention's plan per token row
 };
 
-// prompts: the batch has, or may have, a sequence of several tokens
-Sizes tensor_sizes(const dyn_layer *L, int T, int max_pages, bool prompts) {
+// prompts: the batch has, or may have, a sequence of several tokens; prefix: it names shared prefixes
+Sizes tensor_sizes(const dyn_layer *L, int T, int max_pages, bool prompts, bool prefix) {
     const dyn_layer_config &c = L->cfg;
     const size_t e = esize(c), t = (size_t)std::max(T, 0);
     const int pairs = c.n_experts ? c.top_k : 1;
@@ -154,6 +158,12 @@ Sizes tensor_sizes(const dyn_layer *L, int T, int max_pages, bool prompts) {
     const dyn::AttnShape sh{c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size, max_pages, L->chunk_pages, z.max_chunks, 0};
     if (prompts && dyn::attention_mfma_supported(c.dtype, sh))
         z.max_chunks = std::max(z.max_chunks, dyn::attn_prefill_max_chunks((long)std::max(max_pages, 1) * c.page_size));
+    z.prefix_chunks = prefix ? dyn::attn_prefix_max_chunks(c.dtype, sh) : 0;
+    // per dispatch: two lists of 2 header words + 2 per entry, one chunk size per token; with shared prefixes three lists and eight arrays of a
+    // word per token
+    const dyn::AttnPrefix shared{nullptr, nullptr, 0, z.prefix_chunks};
+    const dyn::AttnShape lists{c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size, max_pages, L->chunk_pages, z.max_chunks, 0};
+    z.plan_row = prefix ? dyn::attn_shared_plan_words(lists, shared, 1) : 4 * ((size_t)z.max_chunks + 2);
     z.h = t * z.ld_h * e;
     z.qkv = t * qkv_width(c) * e;
     z.attn = t * z.ld_attn * e;
@@ -164,7 +174,7 @@ Sizes tensor_sizes(const dyn_layer *L, int T, int max_pages, bool prompts) {
     z.act = t * pairs * z.ld_act * e;
     z.xa = c.n_layers > 1 ? t * c.hidden * e : 0;
     z.xb = c.n_layers > 2 ? t * c.hidden * e : 0;
-    z.plan = (t * z.max_chunks + 2 * t) * 4 * sizeof(int32_t);   // per dispatch: two lists of 2 header words + 2 per entry, one chunk size per token
+    z.plan = t * z.plan_row * sizeof(int32_t);
     z.sel = c.n_experts ? t * c.top_k * sizeof(int32_t) : 0;
     z.wgt = c.n_experts ? t * c.top_k * sizeof(float) : 0;
     return z;
@@ -193,8 +203,8 @@ ScratchBytes dispatch_scratch(const dyn_layer *L, const Sizes &z, const Dispatch
         case DYN_OP_QKV: k.planes = planes(NQKV, H); break;
         case DYN_OP_OPROJ: k.planes = planes(H, NQ); break;
         case DYN_OP_ATTN:
-            k.part_o = r * c.n_q_heads * z.max_chunks * c.head_dim * sizeof(float);
-            k.part_ml = r * c.n_q_heads * z.max_chunks * 2 * sizeof(float);
+            k.part_o = r * c.n_q_heads * (z.max_chunks + z.prefix_chunks) * c.head_dim * sizeof(float);
+            k.part_ml = r * c.n_q_heads * (z.max_chunks + z.prefix_chunks) * 2 * sizeof(float);
             break;
         case DYN_OP_GATE_UP:
             if (moe) {
@@ -221,9 +231,9 @@ ScratchBytes dispatch_scratch(const dyn_layer *L, const Sizes &z, const Dispatch
 // Upper bound of the workspace any legal schedule of a batch of T tokens needs: every tensor and,
 // for every operator, scratch for all T rows at once (a schedule dispatches each (operator,
 // micro-batch) once per layer, so its dispatches' scratch adds up to at most that), nothing shared.
-size_t ws_bound(const dyn_layer *L, int T, int max_pages) {
+size_t ws_bound(const dyn_layer *L, int T, int max_pages, bool prefix) {
     const dyn_layer_config &c = L->cfg;
-    const Sizes z = tensor_sizes(L, T, max_pages, T > 1);
+    const Sizes z = tensor_sizes(L, T, max_pages, T > 1, prefix);
     const size_t t = (size_t)std::max(T, 0);
     const int pairs = c.n_experts ? c.top_k : 1;
     size_t total = 0;
@@ -235,7 +245,8 @@ size_t ws_bound(const dyn_layer *L, int T, int max_pages) {
         const size_t prow = (i == 2 ? (size_t)pairs : 1) * t;     // the MoE gate/up projection has a row per (token, expert)
         total += align_up(S > 1 ? (size_t)S * prow * widths[i][0] * sizeof(float) : 0);
     }
-    total += align_up(t * c.n_q_heads * z.max_chunks * c.head_dim * sizeof(float)) + align_up(t * c.n_q_heads * z.max_chunks * 2 * sizeof(float));
+    const size_t chunks = (size_t)z.max_chunks + z.prefix_chunks;
+    total += align_up(t * c.n_q_heads * chunks * c.head_dim * sizeof(float)) + align_up(t * c.n_q_heads * chunks * 2 * sizeof(float));
     if (c.n_experts) {
         const int Sd = dyn::gemm_split_k(c.dtype, c.hidden, c.mlp_inter, c.n_experts);
         total += 2 * align_up(t * c.top_k * 2 * c.n_experts * sizeof(int32_t)) + align_up((size_t)Sd * t * c.top_k * c.hidden * sizeof(float));
@@ -461,7 +472,7 @@ dyn_status build_plan(const dyn_layer *L, const dyn_batch *b, const dyn_schedule
     // first layer's attention does.
     for (int i = 0; i < n_slots; ++i) {
         Dispatch &d = plan[i];
-        if (d.op != DYN_OP_ATTN || d.r1 <= d.r0) continue;
+        if (d.op != DYN_OP_ATTN || d.r1 <= d.r0 || b->prefix_lead) continue;       // shared prefixes: lists of another kind
         for (int j = 0; j < n_slots; ++j)
             if (plan[j].op == DYN_OP_NORM1 && plan[j].r0 == d.r0 && plan[j].r1 == d.r1) plan[j].plan = d.plan = true;
     }
@@ -513,9 +524,9 @@ std::vector<int> alive_until(const std::vector<Dispatch> &plan) {
 // overlapping that Section 2.1 names.
 WsLayout plan_layout(const dyn_layer *L, const dyn_batch *b, const std::vector<Dispatch> &plan, std::vector<Region> *regions_out) {
     const dyn_layer_config &c = L->cfg;
-    const Sizes z = tensor_sizes(L, b->n_tokens, b->max_pages_per_seq, b->n_tokens > b->n_seqs);
+    const Sizes z = tensor_sizes(L, b->n_tokens, b->max_pages_per_seq, b->n_tokens > b->n_seqs, b->prefix_lead != nullptr);
     WsLayout w{};
-    w.ld_h = z.ld_h; w.ld_attn = z.ld_attn; w.ld_act = z.ld_act; w.max_chunks = z.max_chunks;
+    w.ld_h = z.ld_h; w.ld_attn = z.ld_attn; w.ld_act = z.ld_act; w.max_chunks = z.max_chunks; w.prefix_chunks = z.prefix_chunks; w.plan_row = z.plan_row;
     const int P = (int)plan.size(), n_slots = P / std::max(c.n_layers, 1);
     w.slot.assign((size_t)std::max(n_slots, 0), SlotScratch{});
     if (P == 0 || n_slots == 0) return w;
@@ -738,7 +749,7 @@ dyn_status launch_op(const dyn_layer *L, const dyn_batch *b, const dyn_schedule 
     dyn::AttnShape sh{c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size, b->max_pages_per_seq, L->chunk_pages, ws.max_chunks, d.n_cus};
     char *kc = b->k_cache_layers ? (char *)b->k_cache_layers[d.layer] : (char *)b->k_cache + (size_t)d.layer * b->kv_layer_stride;
     char *vc = b->v_cache_layers ? (char *)b->v_cache_layers[d.layer] : (char *)b->v_cache + (size_t)d.layer * b->kv_layer_stride;
-    int32_t *const plan = (int32_t *)(base + ws.plan) + (size_t)d.r0 * (ws.max_chunks + 2) * 4;   // attention work lists of these rows
+    int32_t *const plan = (int32_t *)(base + ws.plan) + (size_t)d.r0 * ws.plan_row;   // attention work lists of these rows
     // the dispatch's own scratch: split-K planes of `rows` rows each
     float *const planes = (float *)(base + sc.planes);
     hipError_t err = hipSuccess;
@@ -771,6 +782,13 @@ dyn_status launch_op(const dyn_layer *L, const dyn_batch *b, const dyn_schedule 
         case DYN_OP_ROPE_KV:
             break;                                                // applied by the qkv projection's dispatch
         case DYN_OP_ATTN:
+            if (b->prefix_lead) {
+                const dyn::AttnPrefix prefix{b->prefix_lead, b->prefix_pages, b->n_seqs, ws.prefix_chunks};
+                err = dyn::launch_attention_shared(c.dtype, rowp(base + ws.qkv, NQKV), NQKV, b->seq_of_token + d.r0, b->pos_of_token + d.r0, b->block_table, kc, vc,
+                                                   (void *)rowp(base + ws.attn, ws.ld_attn), ws.ld_attn, (float *)(base + sc.part_o),
+                                                   (float *)(base + sc.part_ml), plan, sh, prefix, rows, st, mid, pre, d.layer > 0);
+                break;
+            }
             err = dyn::launch_attention(c.dtype, rowp(base + ws.qkv, NQKV), b->seq_of_token + d.r0, b->pos_of_token + d.r0,
                                         b->block_table, kc, vc, (void *)rowp(base + ws.attn, ws.ld_attn), ws.ld_attn,
                                         (float *)(base + sc.part_o), (float *)(base + sc.part_ml),
@@ -987,7 +1005,8 @@ std::vector<unsigned char> graph_key(const dyn_batch *b, const dyn_schedule *s, 
         const unsigned char *c = (const unsigned char *)p;
         key.insert(key.end(), c, c + n);
     };
-    const void *ptrs[] = {b->x, b->y, b->seq_of_token, b->pos_of_token, b->block_table, b->k_cache, b->v_cache, b->workspace};
+    const void *ptrs[] = {b->x, b->y, b->seq_of_token, b->pos_of_token, b->block_table, b->k_cache, b->v_cache, b->workspace,
+                          b->prefix_lead, b->prefix_pages};
     put(ptrs, sizeof ptrs);
     const int64_t dims[] = {b->n_tokens, b->n_seqs, b->max_pages_per_seq, (int64_t)b->kv_layer_stride,
                             (int64_t)b->workspace_bytes, (int64_t)plan.size()};
@@ -1016,7 +1035,7 @@ void analyse_memory(const dyn_layer *L, const dyn_batch *b, const std::vector<Di
                     dyn_memory_report *out, size_t *peak, int *peak_at) {
     const dyn_layer_config &c = L->cfg;
     const size_t e = esize(c);
-    const Sizes ws = tensor_sizes(L, b->n_tokens, b->max_pages_per_seq, b->n_tokens > b->n_seqs);
+    const Sizes ws = tensor_sizes(L, b->n_tokens, b->max_pages_per_seq, b->n_tokens > b->n_seqs, b->prefix_lead != nullptr);
     const int n_slots = (int)plan.size() / c.n_layers;
     const bool moe = c.n_experts > 0, gated = plan_gated(c, plan);                        // as plan_layout
     const bool norm1 = !norm_in(plan, DYN_OP_QKV), norm2 = !norm_in(plan, DYN_OP_GATE_UP);
@@ -1078,7 +1097,7 @@ void analyse_memory(const dyn_layer *L, const dyn_batch *b, const std::vector<Di
             case DYN_OP_QKV: scratch[i] = planes(NQKV, H); break;
             case DYN_OP_OPROJ: scratch[i] = planes(H, NQ); break;
             case DYN_OP_ATTN:
-                scratch[i] = r * c.n_q_heads * ws.max_chunks * (c.head_dim + 2) * sizeof(float) + (r * ws.max_chunks + 2 * r) * 4 * sizeof(int32_t);
+                scratch[i] = r * c.n_q_heads * (ws.max_chunks + ws.prefix_chunks) * (c.head_dim + 2) * sizeof(float) + r * ws.plan_row * sizeof(int32_t);
                 break;
             case DYN_OP_GATE_UP:
                 scratch[i] = moe ? lists + (gated ? 0 : (size_t)dyn::gemm_split_k(c.dtype, 2 * I, H, c.n_experts) > 1
@@ -1160,6 +1179,9 @@ dyn_status check_batch_tensors(const dyn_layer *L, const dyn_batch *b) {
     if (!b->x || !b->y || !b->seq_of_token || !b->pos_of_token || !b->block_table)
         return fail(DYN_ERR_INVALID_ARG, "NULL tensor pointer in batch");
     if (b->x == b->y) return fail(DYN_ERR_INVALID_ARG, "y must not alias x");
+    if ((b->prefix_lead != nullptr) != (b->prefix_pages != nullptr)) return fail(DYN_ERR_INVALID_ARG, "prefix_lead and prefix_pages go together");
+    if (b->prefix_lead && (long long)b->n_seqs * b->max_pages_per_seq >= 1 << 29)
+        return fail(DYN_ERR_UNSUPPORTED, "shared prefixes need a block table of less than 2^29 entries");
     if ((b->k_cache_layers != nullptr) != (b->v_cache_layers != nullptr))
         return fail(DYN_ERR_INVALID_ARG, "k_cache_layers and v_cache_layers go together");
     if (b->k_cache_layers) {
@@ -1219,7 +1241,7 @@ void dyn_layer_destroy(dyn_layer *L) {
 
 size_t dyn_layer_workspace_bytes(const dyn_layer *L, int max_tokens, int max_pages_per_seq) {
     if (!L || max_tokens < 0 || max_pages_per_seq < 0) return 0;
-    return ws_bound(L, max_tokens, max_pages_per_seq);
+    return ws_bound(L, max_tokens, max_pages_per_seq, false);
 }
 
 dyn_status dyn_schedule_validate(const dyn_layer *L, const dyn_batch *b, const dyn_schedule *s) {
@@ -1256,7 +1278,7 @@ dyn_status dyn_schedule_memory(const dyn_layer *L, const dyn_batch *b, const dyn
     dyn_status rc = build_plan(L, b, s, plan);
     if (rc != DYN_OK) return rc;
     *out = dyn_memory_report{};
-    out->workspace_bytes = ws_bound(L, b->n_tokens, b->max_pages_per_seq);
+    out->workspace_bytes = ws_bound(L, b->n_tokens, b->max_pages_per_seq, b->prefix_lead != nullptr);
     out->workspace_bytes_schedule = plan_layout(L, b, plan, nullptr).total;
     if (b->n_tokens == 0) return DYN_OK;
     const int32_t whole[2] = {0, b->n_tokens};

@@ -12,6 +12,7 @@
 // positions; attn_generic_kernel (one wave per (token, q head, chunk), plain loops) takes the rest.
 #include <algorithm>
 
+#include "attn_shared.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -85,7 +86,7 @@ struct TileList {
 #pragma unroll
         for (int i = 0; i < kRowsPerThread; ++i) {
             const bool ends = r0 + i + 1 >= rows || seq[i + 1] != seq[i] || quotient(pos[i + 1], rule.per_block) != quotient(pos[i], rule.per_block);
-            if (r0 + i < rows && ends) n += quotient(pos[i], rule.per_chunk) + 1;
+            if (r0 + i < rows && ends && pos[i] >= 0) n += quotient(pos[i], rule.per_chunk) + 1;
             upto[i] = n;
         }
         int incl = n;
@@ -123,11 +124,13 @@ struct TileList {
     }
 };
 
-template <typename T, int HD, int TP>
+// PARTS: every item leaves partials for a merge of its own (kernels_attn_shared.hip), q rows are ld_q apart, and the bits of a sequence number above kTileSeq say how its group is served: kTileWide as
+// several tokens, however many are left of it, kTileNarrow by quarters of the chunk, up to 16 columns of them; the sign only tells adjacent groups apart.
+template <typename T, int HD, int TP, bool PARTS>
 __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32_t *__restrict__ block_table, const T *__restrict__ k_cache,
                                           const T *__restrict__ v_cache, T *__restrict__ out, int ld_out, float *__restrict__ part_o,
                                           float *__restrict__ part_ml, const AttnShape &sh, const TileRule &rule, const TileItem &item,
-                                          float (*merge_o)[16][(HD < 128 ? HD : 128) + 4], float (*merge_ml)[16][2]) {
+                                          float (*merge_o)[16][(HD < 128 ? HD : 128) + 4], float (*merge_ml)[16][2], int ld_q) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NK = F32 ? HD / 16 : HD / 32, ND = HD / 16;      // 16-byte K operands and 16-row V operands of a lane
     constexpr int MD = HD < 128 ? HD : 128;                        // head-dim indices merged per round
@@ -138,12 +141,13 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
     const int G = rule.G, TG = rule.TG, tg = rule.block;           // tokens per set of columns, per group
     const int col_tok = (lr * rule.g_mul) >> 16, col_head = lr - col_tok * G;   // this lane's column: a token of the wave's set and a q head
     const int s = item.seq, p_last = item.pos, row_seq = item.row_seq, row_pos = item.row_pos;
-    const int n_tok = __popcll(__ballot(lane < tg && lane <= item.t_last && row_seq == s && quotient(row_pos, rule.per_block) == quotient(p_last, rule.per_block)));
+    const unsigned long long alike = __ballot(lane < tg && lane <= item.t_last && row_seq == s && quotient(row_pos, rule.per_block) == quotient(p_last, rule.per_block));
+    const int n_tok = PARTS ? (~alike ? __ffsll(~alike) - 1 : 64) : __popcll(alike);          // (a run that others cut has rows like these farther back)
     const int t = item.t_last - n_tok + 1, n_keys = p_last + 1;    // the group's first token; keys its last token attends
     const int ps = sh.page_size, ct = rule.chunk, j0 = c * ct;
     const int j1 = min(j0 + ct, n_keys);
-    const bool single = n_tok == 1;
-    const int32_t *bt = block_table + (size_t)s * sh.max_pages_per_seq;
+    const bool single = PARTS && (s & (kTileWide | kTileNarrow)) ? (s & kTileNarrow) != 0 : n_tok == 1;
+    const int32_t *bt = block_table + (size_t)(PARTS ? s & kTileSeq : s) * sh.max_pages_per_seq;
     const float tiles_per_page = 16.0f / (float)ps;
 
     const int set0 = single ? 0 : wave * TG;                       // first token of the wave's columns
@@ -151,7 +155,7 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
     const int col_pos = __shfl(row_pos, max(n_tok - 1 - set0 - min(col_tok, TG - 1), 0), 64);   // every lane takes part
     const int col_keys = live ? col_pos + 1 : 0;                   // keys the column attends
     u32x4 qf[NK];
-    const T *qp = qkv + (size_t)(t + (live ? set0 + col_tok : 0)) * ((sh.n_q + 2 * sh.n_kv) * HD) + (size_t)(g * G + (live ? col_head : 0)) * HD;
+    const T *qp = qkv + (size_t)(t + (live ? set0 + col_tok : 0)) * (PARTS ? ld_q : (sh.n_q + 2 * sh.n_kv) * HD) + (size_t)(g * G + (live ? col_head : 0)) * HD;
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
         qf[k] = *reinterpret_cast<const u32x4 *>(qp + (F32 ? k * 16 + 4 * lq : k * 32 + 8 * lq));
@@ -380,7 +384,7 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
         const ColumnEnd end = column_end(col_keys, j0, ct);
         if (end == COLUMN_NOT_MINE) return;
         const int tq = t + set0 + col_tok, h = g * G + col_head;
-        if (end == COLUMN_DONE) {
+        if (!PARTS && end == COLUMN_DONE) {
             const float inv = 1.0f / l_run;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) store4(out + (size_t)tq * ld_out + h * HD + dt * 16 + 4 * lq, acc[dt] * inv);
@@ -406,8 +410,8 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
             if (dt / (MD / 16) == round) *reinterpret_cast<f32x4 *>(&merge_o[wave][lr][(dt % (MD / 16)) * 16 + 4 * lq]) = acc[dt] * mine;
         if (round == 0 && lq == 0) merge_ml[wave][lr][1] = l_run * mine;
         __syncthreads();
-        for (int u = threadIdx.x; u < G * (MD / 4); u += 256) {
-            const int col = u / (MD / 4), i = (u % (MD / 4)) * 4, h = g * G + col;
+        for (int u = threadIdx.x; u < (PARTS ? n_tok * G : G) * (MD / 4); u += 256) {
+            const int col = u / (MD / 4), i = (u % (MD / 4)) * 4, tok = PARTS ? (col * rule.g_mul) >> 16 : 0, h = g * G + col - tok * G;
             f32x4 o = *reinterpret_cast<const f32x4 *>(&merge_o[0][col][i]);
             float L = merge_ml[0][col][1];
 #pragma unroll
@@ -417,10 +421,10 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
                 L += merge_ml[w][col][1];
             }
             const int d = round * MD + i;
-            if (n_keys <= ct) {
+            if (!PARTS && n_keys <= ct) {
                 store4(out + (size_t)t * ld_out + h * HD + d, o * (1.0f / L));
             } else {
-                const size_t pidx = part_index(sh, t, h, c);
+                const size_t pidx = part_index(sh, t + tok, h, c);
                 *reinterpret_cast<f32x4 *>(part_o + pidx * HD + d) = o;
                 if (d == 0) {
                     float Mh = -INFINITY;
@@ -436,13 +440,13 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
 
 // LIST: the workgroups walk the items that exist, dealt in turn; else one workgroup per (chunk, kv head, token) of the
 // dense grid, of which only a group's last token and the chunks it reaches have work.
-template <typename T, int HD, int TP, bool LIST>
+template <typename T, int HD, int TP, bool LIST, bool PARTS>
 __global__ __launch_bounds__(256, HD * sizeof(T) <= 256 ? 2 : 1) void attn_tile_kernel(const T *__restrict__ qkv, const int32_t *__restrict__ seq_of_token,
                                                         const int32_t *__restrict__ pos_of_token,
                                                         const int32_t *__restrict__ block_table, const T *__restrict__ k_cache,
                                                         const T *__restrict__ v_cache, T *__restrict__ out, int ld_out,
                                                         float *__restrict__ part_o, float *__restrict__ part_ml, AttnShape sh,
-                                                        TileRule rule, int rows, int y0, int y1) {
+                                                        TileRule rule, int rows, int y0, int y1, int ld_q) {
     __shared__ float merge_o[4][16][(HD < 128 ? HD : 128) + 4];
     __shared__ float merge_ml[4][16][2];
     auto item_of = [&](int t_last, int c, int g) {
@@ -450,7 +454,7 @@ __global__ __launch_bounds__(256, HD * sizeof(T) <= 256 ? 2 : 1) void attn_tile_
         return TileItem{t_last, c, g, seq_of_token[t_last], pos_of_token[t_last], seq_of_token[row], pos_of_token[row]};
     };
     auto serve = [&](const TileItem &item) {
-        attn_tile<T, HD, TP>(qkv, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rule, item, merge_o, merge_ml);
+        attn_tile<T, HD, TP, PARTS>(qkv, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rule, item, merge_o, merge_ml, ld_q);
     };
     if constexpr (LIST) {
         __shared__ int scratch[8];
@@ -498,7 +502,7 @@ __global__ __launch_bounds__(64) void attn_generic_kernel(const T *__restrict__ 
                                                           const int32_t *__restrict__ block_table,
                                                           const T *__restrict__ k_cache, const T *__restrict__ v_cache,
                                                           float *__restrict__ part_o, float *__restrict__ part_ml,
-                                                          AttnShape sh) {
+                                                          AttnShape sh, int ld_q) {
     const int c = blockIdx.x % sh.max_chunks;
     const int h = (blockIdx.x / sh.max_chunks) % sh.n_q;
     const int t = blockIdx.x / (sh.max_chunks * sh.n_q);
@@ -513,7 +517,7 @@ __global__ __launch_bounds__(64) void attn_generic_kernel(const T *__restrict__ 
 
     __shared__ float qs[2 * kMaxHalfDim];
     __shared__ float sc[kMaxChunkTokens];
-    const T *q = qkv + (size_t)t * ((sh.n_q + 2 * sh.n_kv) * d) + h * d;
+    const T *q = qkv + (size_t)t * ld_q + h * d;
     for (int i = lane; i < d; i += 64) qs[i] = to_f32<T>(q[i]);
     __syncthreads();
 
@@ -845,17 +849,17 @@ constexpr size_t kGeneralGrid = (size_t)1 << 25;       // of the general form
 constexpr size_t kListGrid = 512;
 
 
-template <typename T, int HD, int TP>
+template <typename T, int HD, int TP, bool PARTS>
 void launch_attn_tile(hipStream_t s, const void *qkv, const int32_t *seq_of_token, const int32_t *pos_of_token,
                       const int32_t *block_table, const void *k_cache, const void *v_cache, void *out, int ld_out, float *part_o,
-                      float *part_ml, const AttnShape &sh, int rows) {
+                      float *part_ml, const AttnShape &sh, int rows, int ld_q) {
     const int n_y = sh.n_kv * sh.max_chunks;
     const size_t dense = (size_t)rows * n_y;
     const int G = sh.n_q / sh.n_kv, block = 4 * (16 / G), chunk = sh.chunk_pages * sh.page_size;
     const TileRule rule{1.0 / block, 1.0 / chunk, 1.0 / sh.n_kv, G, 16 / G, block, chunk, 65536 / G + 1};
 #define DYN_TILE_LAUNCH(LIST, GRID, Y0, Y1)                                                                                              \
-    hipLaunchKernelGGL((attn_tile_kernel<T, HD, TP, LIST>), dim3(GRID), dim3(256), 0, s, (const T *)qkv, seq_of_token, pos_of_token,     \
-                       block_table, (const T *)k_cache, (const T *)v_cache, (T *)out, ld_out, part_o, part_ml, sh, rule, rows, Y0, Y1)
+    hipLaunchKernelGGL((attn_tile_kernel<T, HD, TP, LIST, PARTS>), dim3(GRID), dim3(256), 0, s, (const T *)qkv, seq_of_token, pos_of_token,     \
+                       block_table, (const T *)k_cache, (const T *)v_cache, (T *)out, ld_out, part_o, part_ml, sh, rule, rows, Y0, Y1, ld_q)
     if (rows <= kListRows && dense > kListGrid) {
         DYN_TILE_LAUNCH(true, (unsigned)std::min<size_t>(dense, HD * sizeof(T) >= 256 ? 512 : 1024), 0, n_y);
         return;
@@ -867,7 +871,61 @@ void launch_attn_tile(hipStream_t s, const void *qkv, const int32_t *seq_of_toke
     }
 #undef DYN_TILE_LAUNCH
 }
+
+hipError_t launch_attn_general(int dtype, hipStream_t s, const void *qkv, const int32_t *seq_of_token, const int32_t *pos_of_token, const int32_t *block_table,
+                               const void *k_cache, const void *v_cache, float *part_o, float *part_ml, const AttnShape &sh, int rows, int ld_q) {
+    const size_t per_row = (size_t)sh.n_q * sh.max_chunks, width = ld_q;
+    const int step = (int)std::max<size_t>(kGeneralGrid / per_row, 1);
+    if (per_row >= (size_t)1 << 26) return hipErrorInvalidConfiguration;
+    for (int r0 = 0; r0 < rows; r0 += std::min(step, rows - r0)) {
+        const dim3 grid((unsigned)(std::min(step, rows - r0) * per_row));
+        float *const po = part_o + part_index(sh, r0, 0, 0) * sh.head_dim, *const pml = part_ml + part_index(sh, r0, 0, 0) * 2;
+        if (dtype == 0)
+            hipLaunchKernelGGL(attn_generic_kernel<float>, grid, dim3(64), 0, s, (const float *)qkv + r0 * width, seq_of_token + r0,
+                               pos_of_token + r0, block_table, (const float *)k_cache, (const float *)v_cache, po, pml, sh, ld_q);
+        else
+            hipLaunchKernelGGL(attn_generic_kernel<bf16_t>, grid, dim3(64), 0, s, (const bf16_t *)qkv + r0 * width, seq_of_token + r0,
+                               pos_of_token + r0, block_table, (const bf16_t *)k_cache, (const bf16_t *)v_cache, po, pml, sh, ld_q);
+    }
+    return hipGetLastError();
+}
+
+template <bool PARTS>
+void launch_attn_tiles(int dtype, hipStream_t s, const void *qkv, const int32_t *seq_of_token, const int32_t *pos_of_token,
+                       const int32_t *block_table, const void *k_cache, const void *v_cache, void *out, int ld_out, float *part_o,
+                       float *part_ml, const AttnShape &sh, int rows, int ld_q) {
+    // positions per tile: two sub-tiles of 16 where a lane's K and V operands of both fit beside the
+    // accumulators twice over, else one
+#define DYN_TILE(T, HD, TP) launch_attn_tile<T, HD, TP, PARTS>(s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rows, ld_q)
+    if (dtype == 0) {
+        switch (sh.head_dim) {
+            case 32: DYN_TILE(float, 32, 2); break;
+            case 64: DYN_TILE(float, 64, 2); break;
+            case 128: DYN_TILE(float, 128, 1); break;
+            default: DYN_TILE(float, 256, 1); break;
+        }
+    } else {
+        switch (sh.head_dim) {
+            case 32: DYN_TILE(bf16_t, 32, 2); break;
+            case 64: DYN_TILE(bf16_t, 64, 2); break;
+            case 128: DYN_TILE(bf16_t, 128, 1); break;
+            default: DYN_TILE(bf16_t, 256, 1); break;
+        }
+    }
+#undef DYN_TILE
+}
 }  // namespace
+
+// Partials, and nothing but partials, of rows described by arrays of their own (kernels_attn_shared.hip).  tile: attn_tile_takes said so.
+bool attn_tile_takes(const AttnShape &sh, const void *k_cache, const void *v_cache) { return attn_tile_supported(sh, k_cache, v_cache); }
+hipError_t launch_attention_parts(int dtype, bool tile, const void *q, int ld_q, const int32_t *seq_of_token, const int32_t *pos_of_token, const int32_t *block_table,
+                                  const void *k_cache, const void *v_cache, float *part_o, float *part_ml, const AttnShape &sh, int rows, hipStream_t s) {
+    if (tile) {
+        launch_attn_tiles<true>(dtype, s, q, seq_of_token, pos_of_token, block_table, k_cache, v_cache, nullptr, 0, part_o, part_ml, sh, rows, ld_q);
+        return hipGetLastError();
+    }
+    return launch_attn_general(dtype, s, q, seq_of_token, pos_of_token, block_table, k_cache, v_cache, part_o, part_ml, sh, rows, ld_q);
+}
 
 hipError_t launch_attention_generic(int dtype, const void *qkv, const int32_t *seq_of_token,
                                     const int32_t *pos_of_token, const int32_t *block_table, const void *k_cache,
@@ -877,39 +935,11 @@ hipError_t launch_attention_generic(int dtype, const void *qkv, const int32_t *s
     if (rows >= 1 << 24) return hipErrorInvalidConfiguration;
     const bool tile = attn_tile_supported(sh, k_cache, v_cache);
     if (tile) {
-        // positions per tile: two sub-tiles of 16 where a lane's K and V operands of both fit beside the
-        // accumulators twice over, else one
-#define DYN_TILE(T, HD, TP) launch_attn_tile<T, HD, TP>(s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rows)
-        if (dtype == 0) {
-            switch (sh.head_dim) {
-                case 32: DYN_TILE(float, 32, 2); break;
-                case 64: DYN_TILE(float, 64, 2); break;
-                case 128: DYN_TILE(float, 128, 1); break;
-                default: DYN_TILE(float, 256, 1); break;
-            }
-        } else {
-            switch (sh.head_dim) {
-                case 32: DYN_TILE(bf16_t, 32, 2); break;
-                case 64: DYN_TILE(bf16_t, 64, 2); break;
-                case 128: DYN_TILE(bf16_t, 128, 1); break;
-                default: DYN_TILE(bf16_t, 256, 1); break;
-            }
-        }
-#undef DYN_TILE
+        launch_attn_tiles<false>(dtype, s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rows, 0);
     } else {
-        const size_t per_row = (size_t)sh.n_q * sh.max_chunks, width = (size_t)(sh.n_q + 2 * sh.n_kv) * sh.head_dim;
-        const int step = (int)std::max<size_t>(kGeneralGrid / per_row, 1);
-        if (per_row >= (size_t)1 << 26) return hipErrorInvalidConfiguration;
-        for (int r0 = 0; r0 < rows; r0 += std::min(step, rows - r0)) {
-            const dim3 grid((unsigned)(std::min(step, rows - r0) * per_row));
-            float *const po = part_o + part_index(sh, r0, 0, 0) * sh.head_dim, *const pml = part_ml + part_index(sh, r0, 0, 0) * 2;
-            if (dtype == 0)
-                hipLaunchKernelGGL(attn_generic_kernel<float>, grid, dim3(64), 0, s, (const float *)qkv + r0 * width, seq_of_token + r0,
-                                   pos_of_token + r0, block_table, (const float *)k_cache, (const float *)v_cache, po, pml, sh);
-            else
-                hipLaunchKernelGGL(attn_generic_kernel<bf16_t>, grid, dim3(64), 0, s, (const bf16_t *)qkv + r0 * width, seq_of_token + r0,
-                                   pos_of_token + r0, block_table, (const bf16_t *)k_cache, (const bf16_t *)v_cache, po, pml, sh);
-        }
+        const hipError_t e = launch_attn_general(dtype, s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, part_o, part_ml, sh, rows,
+                                                 (sh.n_q + 2 * sh.n_kv) * sh.head_dim);
+        if (e != hipSuccess) return e;
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && mid) e = hipEventRecord(mid, s);

@@ -1,0 +1,351 @@
+// Attention of a batch whose sequences share prefixes: the shared pages are read once for all that share them.
+//
+// A token at position p attends keys 0 .. p of its sequence.  Softmax over two sets of keys is that of each, merged:
+//     m = max(m1, m2),  o = (e^(m1 - m) o1 + e^(m2 - m) o2) / (e^(m1 - m) l1 + e^(m2 - m) l2)
+// with o_i, l_i the sums of e^(s - m_i) v and e^(s - m_i) over set i.  So the first P keys, which many sequences have in common, become
+// one attention of all their tokens against the same pages - a product with many columns, as a prompt's - and the keys behind
+// them an attention of every sequence for itself, as a decode's or a prompt's that starts at P.  Three launches: the plan
+// (kernels_attn_shared_plan.hip), the keys (attn_shared_kernel, or attn_tile of kernels_attn_generic.hip for what it does not
+// take), and the merge of a row's chunks.
+#include <algorithm>
+
+#include "attn_prefill.h"
+#include "attn_shared_plan.h"
+#include "common.h"
+
+namespace dyn {
+
+namespace {
+
+constexpr int HD = 128, TILE = 2;         // head dim; sub-tiles of 16 positions (pages) to a register buffer
+
+struct SharedArgs {
+    const bf16_t *q, *k, *v;
+    const int32_t *block_table;
+    SharedPlan plan;
+    AttnShape sh;                         // rows of a table of one wide row; max_chunks: of both halves
+    int ld_q, shared_slots;               // partials of own keys lie behind shared_slots chunks of shared ones
+    int few_subs, own_subs;               // sub-tiles per chunk of an item: of shared and of own keys
+    float *part_o, *part_ml;
+};
+
+// One wave's work: up to 16 columns (a token and a q head each) against one chunk of one kv head, all of them seeing all of it.
+struct Item {
+    int t, n_tok, own, c, g;              // first token row, tokens, whose keys, chunk, kv head
+    int first, last, end;                 // the chunk's sub-tiles; the first position past it
+    const int32_t *table;
+};
+
+// The items, dealt to n_blocks workgroups of WAVES waves.  K and V go from memory straight into MFMA operand layout,
+//     S[16 pos, 16 cols]  = K_sub[16, 128] Q^T[128, 16]       (4 x mfma 16x16x32 per sub-tile)
+//     O^T[128, 16 cols]  += V^T[128, 32] P[32, 16]            (8 x mfma 16x16x32 per pair of sub-tiles)
+// with the D layout of the first product (lane: column l % 16, positions 4 (l / 16) + r) the B layout of the second.  Two register
+// buffers of 32 positions; the last pair of a chunk is followed by the first of the wave's next item, whose indices were
+// fetched while this one was multiplied.
+template <int WAVES>
+__device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int n_blocks) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnShape &sh = a.sh;
+    const int n_items = a.plan.items[0] * sh.n_kv, n_waves = n_blocks * WAVES;
+    const int G = sh.n_q / sh.n_kv, col_tok = lr / G, col_head = lr - col_tok * G;
+    const float scale = 1.4426950408889634f / sqrtf((float)HD);        // log2(e) / sqrt(d)
+    // few rounds: a wave of every workgroup first (what a CU gets from memory is bounded per CU)
+    const int gw = n_items < 4 * n_waves ? wave * n_blocks + block : block * WAVES + wave;
+    int round = 0;
+    auto item_at = [&](int k) { return k * n_waves + ((k & 1) ? n_waves - 1 - gw : gw); };
+    if (item_at(0) >= n_items) return;
+
+    auto fetch = [&](int i) {
+        Item m;
+        const int e = i / sh.n_kv, row = a.plan.items[2 + 2 * e], packed = a.plan.items[3 + 2 * e];
+        m.g = i - e * sh.n_kv;
+        m.t = row & (kOwnItem - 1);
+        m.own = row >> 30;
+        m.c = packed & 0xfffff;
+        m.n_tok = packed >> 20;
+        const int keys = (m.own ? a.plan.s_pos : a.plan.p_pos)[m.t] + 1;
+        m.table = a.block_table + (m.own ? a.plan.s_seq : a.plan.p_seq)[m.t];
+        // chunks of equal size up to rounding, a function of the half's own length
+        const int subs = (keys + 15) >> 4, most = m.own ? a.own_subs : a.few_subs, n = (subs + most - 1) / most, per = (subs + n - 1) / n;
+        m.first = m.c * per;
+        m.last = min(m.first + per, subs) - 1;
+        m.end = min(keys, (m.last + 1) * 16);
+        return m;
+    };
+    u32x4 kr[2][TILE][4];
+    u32x2 vr[2][TILE][8];
+    bf16x8 q[4], q_next[4];
+    auto load = [&](auto buf, const Item &m, int tile) {
+        constexpr int B = decltype(buf)::value;
+#pragma unroll
+        for (int i = 0; i < TILE; ++i) {
+            const size_t page = (size_t)m.table[min(m.first + tile * TILE + i, m.last)] * sh.n_kv + m.g;
+            const bf16_t *kp = a.k + (page * 16 + lr) * HD + 8 * lq, *vp = a.v + (page * HD + lr) * 16 + 4 * lq;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) kr[B][i][ks] = *reinterpret_cast<const u32x4 *>(kp + ks * 32);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) vr[B][i][dt] = *reinterpret_cast<const u32x2 *>(vp + dt * 256);
+        }
+    };
+    auto load_q = [&](bf16x8 (&dst)[4], const Item &m) {
+        const bool live = col_tok < m.n_tok;
+        const bf16_t *qp = a.q + (size_t)(m.t + (live ? col_tok : 0)) * a.ld_q + (m.g * G + col_head) * HD + 8 * lq;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            u32x4 x = *reinterpret_cast<const u32x4 *>(qp + ks * 32);
+            if (!live) x = u32x4{0u, 0u, 0u, 0u};
+            dst[ks] = __builtin_bit_cast(bf16x8, x);
+        }
+    };
+    f32x4 acc[8];
+    float m_run, l_run;
+    auto multiply = [&](auto buf, const Item &m, int tile) {
+        constexpr int B = decltype(buf)::value;
+        const int at = (m.first + tile * TILE) * 16;
+        f32x4 s[TILE];
+#pragma unroll
+        for (int i = 0; i < TILE; ++i) {
+            s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[B][i][ks]), q[ks], s[i], 0, 0, 0);
+            s[i] *= scale;
+        }
+        if (at + 16 * TILE > m.end) {                                    // the chunk ends in this tile (wave-uniform)
+#pragma unroll
+            for (int i = 0; i < TILE; ++i) {
+                const int n = m.end - (at + 16 * i + 4 * lq);            // valid positions of this lane's four
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (r >= n) s[i][r] = -INFINITY;
+                // what lies past them must not meet its zero probability (0 * NaN)
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    vr[B][i][dt][0] &= (n > 0 ? 0x0000ffffu : 0u) | (n > 1 ? 0xffff0000u : 0u);
+                    vr[B][i][dt][1] &= (n > 2 ? 0x0000ffffu : 0u) | (n > 3 ? 0xffff0000u : 0u);
+                }
+            }
+        }
+        float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+#pragma unroll
+        for (int i = 1; i < TILE; ++i) mx = fmaxf(mx, fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])));
+        mx = prefill::quad_max(mx);
+        const float m_new = fmaxf(m_run, mx), ref = m_new == -INFINITY ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m_run - ref);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) acc[dt] *= alpha;
+        // probabilities are rounded to bf16 for the matrix product, and the same rounded ones are summed
+        u32x2 w[TILE];
+#pragma unroll
+        for (int i = 0; i < TILE; ++i) {
+            f32x4 p;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[i][r] - ref);
+            w[i] = __builtin_bit_cast(u32x2, __builtin_convertvector(p, prefill::bf16x4));
+            l_run += (__uint_as_float(w[i][0] << 16) + __uint_as_float(w[i][0] & 0xffff0000u)) + (__uint_as_float(w[i][1] << 16) + __uint_as_float(w[i][1] & 0xffff0000u));
+        }
+#pragma unroll
+        for (int i = 0; i < TILE; i += 2) {
+            const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{w[i][0], w[i][1], w[i + 1][0], w[i + 1][1]});
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+                const u32x2 x = vr[B][i][dt], y = vr[B][i + 1][dt];
+                acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}), pb, acc[dt], 0, 0, 0);
+            }
+        }
+    };
+    const std::integral_constant<int, 0> b0;
+    const std::integral_constant<int, 1> b1;
+    Item cur = fetch(item_at(0));
+    load_q(q, cur);
+    load(b0, cur, 0);
+    while (true) {
+        const bool more = item_at(round + 1) < n_items;
+        const Item nxt = fetch(item_at(more ? round + 1 : round));       // the last one "prefetches" itself: harmless loads, no branch
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m_run = -INFINITY;
+        l_run = 0.f;
+        const int pairs = (cur.last - cur.first + 2 * TILE) / (2 * TILE);     // an odd tile at the end is walked masked
+        for (int pr = 0; pr < pairs; ++pr) {
+            load(b1, cur, 2 * pr + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(b0, cur, 2 * pr);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool last = pr + 1 == pairs;
+            load_q(q_next, nxt);
+            load(b0, last ? nxt : cur, last ? 0 : 2 * pr + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(b1, cur, 2 * pr + 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        float l = l_run;
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (col_tok < cur.n_tok) {
+            const size_t at = part_index(sh, cur.t + col_tok, cur.g * G + col_head, cur.own ? a.shared_slots + cur.c : cur.c);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4 *>(a.part_o + at * HD + dt * 16 + 4 * lq) = acc[dt];
+            if (lq == 0) {
+                a.part_ml[at * 2] = m_run;
+                a.part_ml[at * 2 + 1] = l;
+            }
+        }
+        if (!more) break;
+        ++round;
+        cur = nxt;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) q[ks] = q_next[ks];
+    }
+}
+
+// Costs in us of one CU, as mixed_prompt_groups (kernels_attn_mfma.hip) has them: a tile of 64 positions of a query block 6, a position of an
+// item 0.026.
+__device__ __forceinline__ float block_cost(const int32_t *list, const int32_t *pos, const int32_t *ct) {
+    const int entries = list[0];
+    if (!entries) return 0.f;
+    auto tiles = [&](int e) {
+        const int t = list[2 + 2 * e], packed = list[3 + 2 * e];
+        return (min(ct[t], pos[t + (packed >> 20) - 1] + 1 - (packed & 0xfffff) * ct[t]) + 63) / 64;
+    };
+    return 1.5f * (tiles(0) + 2 * tiles(entries / 2) + tiles(entries - 1)) * entries;
+}
+
+// All keys of a dispatch in one launch, a workgroup of eight waves per CU: the first claim query blocks (of shared keys, then of own
+// ones), the others serve the items of both and then claim query blocks too.  Items wait for memory and query blocks for the matrix
+// cores (attn_mixed_kernel, kernels_attn_mfma.hip).
+__global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(SharedArgs a) {
+    const SharedPlan &w = a.plan;
+    const float blocks = block_cost(w.p_blocks, w.p_pos, w.p_ct) + block_cost(w.s_blocks, w.s_pos, w.s_ct);
+    const float items = 0.026f * 16 * a.own_subs * w.items[0];
+    const int groups = gridDim.x;
+    const int first = blocks == 0.f ? 0 : items == 0.f ? groups : mixed_share((w.p_blocks[0] + w.s_blocks[0]) * a.sh.n_kv, blocks, items, groups);
+    if ((int)blockIdx.x >= first) serve_items<prefill::kWaves>(a, (int)blockIdx.x - first, groups - first);
+    const size_t behind = part_index(a.sh, 0, 0, a.shared_slots);
+#pragma clang loop unroll(disable)
+    for (int own = 0; own < 2; ++own) {
+        int32_t *const list = own ? w.s_blocks : w.p_blocks;
+        prefill::attn_prefill_items<true>(a.q, own ? w.s_seq : w.p_seq, own ? w.s_pos : w.p_pos, a.block_table, a.k, a.v, nullptr, 0,
+                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q);
+    }
+}
+
+// Merge of a row's partials, shared chunks first, in order: a half-wave per (token, q head), four head-dim indices to a lane (two sets of
+// them beyond 128).  A row without keys is zero.  ct null: chunks of `chunk` positions.
+template <typename T, bool BASE2>
+__global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
+                                                                  const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
+                                                                  const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct, int chunk,
+                                                                  int shared_slots, T *__restrict__ out, int ld_out, AttnShape sh,
+                                                                  int32_t *__restrict__ counter0, int32_t *__restrict__ counter1) {
+    // the lists' query blocks have all been claimed: from the start again for the next layer
+    if (counter0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) *(threadIdx.x ? counter1 : counter0) = 0;
+    const int t = blockIdx.x, sub = threadIdx.x & 31, h = blockIdx.y * 8 + (threadIdx.x >> 5), d = sh.head_dim;
+    if (h >= sh.n_q) return;
+    const int pc = p_ct ? p_ct[t] : chunk, sc = s_ct ? s_ct[t] : chunk;
+    const int n_shared = p_pos[t] < 0 ? 0 : (p_pos[t] + pc) / pc, n_own = s_pos[t] < 0 ? 0 : (s_pos[t] + sc) / sc, n = n_shared + n_own;
+    T *const y = out + (size_t)t * ld_out + h * d;
+    auto at = [&](int c) { return part_index(sh, t, h, c < n_shared ? c : shared_slots + c - n_shared); };
+    float M = -INFINITY;
+    for (int c = sub; c < n; c += 32) M = fmaxf(M, part_ml[at(c) * 2]);
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 32));
+    float L = 0.f;
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    for (int cb = 0; cb < n; cb += 32) {
+        const int c = cb + sub;
+        float wgt = 0.f, wl = 0.f;
+        if (c < n) {
+            const float dm = part_ml[at(c) * 2] - M;
+            wgt = BASE2 ? exp2f(dm) : expf(dm);
+            wl = wgt * part_ml[at(c) * 2 + 1];
+        }
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) wl += __shfl_xor(wl, off, 32);
+        L += wl;
+        const int nb = min(32, n - cb);
+        for (int j0 = 0; j0 < nb; j0 += 8) {
+            f32x4 v[8][2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int i = sub * 4 + k * 128;
+                    v[j][k] = (j0 + j < nb && i < d) ? *reinterpret_cast<const f32x4 *>(part_o + at(cb + j0 + j) * d + i) : f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float wj = __shfl(wgt, j0 + j, 32);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) acc[k] += v[j][k] * wj;
+            }
+        }
+    }
+    const float inv = n ? 1.0f / L : 0.f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = sub * 4 + k * 128;
+        if (i < d) {
+            if constexpr (sizeof(T) == 2) {
+                u32x2 w;
+                w[0] = (uint32_t)f2bf(acc[k][0] * inv) | ((uint32_t)f2bf(acc[k][1] * inv) << 16);
+                w[1] = (uint32_t)f2bf(acc[k][2] * inv) | ((uint32_t)f2bf(acc[k][3] * inv) << 16);
+                *reinterpret_cast<u32x2 *>(y + i) = w;
+            } else {
+                *reinterpret_cast<f32x4 *>(y + i) = acc[k] * inv;
+            }
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int32_t *seq_of_token, const int32_t *pos_of_token, const int32_t *block_table,
+                                   const void *k_cache, const void *v_cache, void *out, int ld_out, float *part_o, float *part_ml, int32_t *plan,
+                                   const AttnShape &sh, const AttnPrefix &prefix, int rows, hipStream_t s, hipEvent_t mid, hipEvent_t pre, bool plan_ready) {
+    if (rows <= 0) return hipSuccess;
+    if (rows >= 1 << 24) return hipErrorInvalidConfiguration;
+    const AttnForm form = attn_shared_form(dtype, sh, k_cache, v_cache);
+    const SharedPlan w = attn_shared_plan(plan, sh, prefix, rows);
+    hipError_t e = plan_ready ? hipSuccess : launch_attn_shared_plan(form, seq_of_token, pos_of_token, sh, prefix, rows, w, s);
+    if (e == hipSuccess && pre) e = hipEventRecord(pre, s);
+    if (e != hipSuccess) return e;
+    AttnShape part = sh;
+    part.max_pages_per_seq = 1;                     // the halves' arrays hold offsets into the table
+    part.max_chunks = sh.max_chunks + prefix.max_chunks;
+    if (form == SHARE_LISTS) {
+        static bool attr_set = false;
+        if (!attr_set) {
+            e = hipFuncSetAttribute((const void *)attn_shared_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, prefill::lds_bytes());
+            if (e != hipSuccess) return e;
+            attr_set = true;
+        }
+        const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, ld_q, prefix.max_chunks, attn_prefix_few_pages(sh),
+                           sh.chunk_pages, part_o, part_ml};
+        const long most = (long)rows * sh.n_kv * part.max_chunks;
+        const int cus = sh.n_cus > 0 && sh.n_cus < 256 ? sh.n_cus : 256;
+        hipLaunchKernelGGL(attn_shared_kernel, dim3((unsigned)std::min<long>(most, cus)), dim3(prefill::kWaves * 64), prefill::lds_bytes(), s, a);
+        e = hipGetLastError();
+    } else {
+        const bool tile = form == SHARE_TILES;
+        const size_t behind = part_index(part, 0, 0, prefix.max_chunks);
+        e = launch_attention_parts(dtype, tile, q, ld_q, w.s_seq, w.s_pos, block_table, k_cache, v_cache, part_o + behind * sh.head_dim, part_ml + behind * 2, part, rows, s);
+        if (e == hipSuccess && tile && prefix.lead)
+            e = launch_attention_parts(dtype, tile, q, ld_q, w.p_seq, w.p_pos, block_table, k_cache, v_cache, part_o, part_ml, part, rows, s);
+    }
+    if (e == hipSuccess && mid) e = hipEventRecord(mid, s);
+    if (e != hipSuccess) return e;
+    const bool lists = form == SHARE_LISTS;
+    const dim3 grid(rows, (sh.n_q + 7) / 8), block(256);
+#define DYN_COMBINE(T, B2)                                                                                                                                     \
+    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2>), grid, block, 0, s, part_o, part_ml, w.p_pos, lists ? w.p_ct : nullptr, w.s_pos,                    \
+                       lists ? w.s_ct : nullptr, sh.chunk_pages * sh.page_size, prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr,  \
+                       lists ? w.s_blocks + 1 : nullptr)
+    if (dtype == 0) DYN_COMBINE(float, false);
+    else if (form != SHARE_NOTHING) DYN_COMBINE(bf16_t, true);
+    else DYN_COMBINE(bf16_t, false);
+#undef DYN_COMBINE
+    return hipGetLastError();
+}
+
+}  // namespace dyn
