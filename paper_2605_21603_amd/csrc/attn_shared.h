@@ -14,13 +14,16 @@ struct AttnPrefix {
     const int32_t *lead = nullptr, *pages = nullptr;
     int n_seqs = 0;
     int max_chunks = 0;          // the most chunks a token's shared keys can have; its own ones are AttnShape::max_chunks
+    const int32_t *seq_of_token = nullptr, *pos_of_token = nullptr;   // all rows of the batch, of which a call may serve some
+    int rows = 0;
 };
 
 // Bits of a row's table offset in the general form's arrays (kernels_attn_generic.hip).
 constexpr int kTileSeq = (1 << 29) - 1, kTileWide = 1 << 29, kTileNarrow = 1 << 30;
 
-// Chunks of the shared keys of a batch whose rows have max_pages pages at most: bounds part_o, part_ml and the lists.
+// The most chunks of a row's shared and of its own keys, of a batch whose rows have sh.max_pages_per_seq pages at most.
 int attn_prefix_max_chunks(int dtype, const AttnShape &sh);
+int attn_own_max_chunks(int dtype, const AttnShape &sh);
 // 32-bit words of scratch for `rows` rows; sh.max_chunks: of the rows' own keys.
 size_t attn_shared_plan_words(const AttnShape &sh, const AttnPrefix &prefix, int rows);
 // As launch_attention, with q rows ld_q elements apart, part_o [rows, sh.max_chunks + prefix.max_chunks, n_q, head_dim] and part_ml to match; a row of position -1 attends

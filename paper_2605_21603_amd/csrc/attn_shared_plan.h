@@ -17,12 +17,13 @@ struct SharedPlan {
     // 16 columns of shared keys, or a single token's own keys (kOwnItem set in the row).  p_blocks, s_blocks: query blocks of shared and
     // of own keys, [1] = the counter that they are claimed from.
     int32_t *items, *p_blocks, *s_blocks;
+    // What the lists take, in us of one CU and kv head: [0] the items, [1] the query blocks.
+    float *cost;
 };
 constexpr int kOwnItem = 1 << 30;
 
 SharedPlan attn_shared_plan(int32_t *plan, const AttnShape &sh, const AttnPrefix &prefix, int rows);
 AttnForm attn_shared_form(int dtype, const AttnShape &sh, const void *k_cache, const void *v_cache);
-int attn_prefix_few_pages(const AttnShape &sh);       // pages per chunk of a prefix that few sequences share
 hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, const int32_t *pos_of_token, const AttnShape &sh, const AttnPrefix &prefix, int rows,
                                    const SharedPlan &w, hipStream_t s);
 

@@ -39,8 +39,8 @@ dyn_status check_sizes(const dyn_attn_batch *b) {
 dyn::AttnShape shape_of(const dyn_attn_batch *b, dyn::AttnPrefix *prefix, Layout *w) {
     const int pages = std::max(b->max_pages_per_seq, 1), chunk = std::max(1, (b->kv_chunk_positions ? b->kv_chunk_positions : 256) / b->page_size);
     dyn::AttnShape sh{b->n_q_heads, b->n_kv_heads, b->head_dim, b->page_size, pages, chunk, (pages + chunk - 1) / chunk, 0};
-    if (dyn::attention_mfma_supported(b->dtype, sh)) sh.max_chunks = std::max(sh.max_chunks, dyn::attn_prefill_max_chunks((long)pages * b->page_size));
-    *prefix = dyn::AttnPrefix{b->prefix_lead, b->prefix_pages, b->n_seqs, dyn::attn_prefix_max_chunks(b->dtype, sh)};
+    sh.max_chunks = dyn::attn_own_max_chunks(b->dtype, sh);
+    *prefix = dyn::AttnPrefix{b->prefix_lead, b->prefix_pages, b->n_seqs, dyn::attn_prefix_max_chunks(b->dtype, sh), b->seq_of_token, b->pos_of_token, b->n_tokens};
     const size_t partials = (size_t)b->n_tokens * b->n_q_heads * (sh.max_chunks + prefix->max_chunks);
     w->part_o = 0;
     w->part_ml = align_up(partials * b->head_dim * sizeof(float));

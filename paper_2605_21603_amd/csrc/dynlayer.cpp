@@ -159,9 +159,10 @@ Sizes tensor_sizes(const dyn_layer *L, int T, int max_pages, bool prompts, bool 
     if (prompts && dyn::attention_mfma_supported(c.dtype, sh))
         z.max_chunks = std::max(z.max_chunks, dyn::attn_prefill_max_chunks((long)std::max(max_pages, 1) * c.page_size));
     z.prefix_chunks = prefix ? dyn::attn_prefix_max_chunks(c.dtype, sh) : 0;
+    if (prefix) z.max_chunks = dyn::attn_own_max_chunks(c.dtype, sh);
     // per dispatch: two lists of 2 header words + 2 per entry, one chunk size per token; with shared prefixes three lists and eight arrays of a
     // word per token
-    const dyn::AttnPrefix shared{nullptr, nullptr, 0, z.prefix_chunks};
+    const dyn::AttnPrefix shared{nullptr, nullptr, 0, z.prefix_chunks, nullptr, nullptr, 0};
     const dyn::AttnShape lists{c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size, max_pages, L->chunk_pages, z.max_chunks, 0};
     z.plan_row = prefix ? dyn::attn_shared_plan_words(lists, shared, 1) : 4 * ((size_t)z.max_chunks + 2);
     z.h = t * z.ld_h * e;
@@ -783,7 +784,7 @@ dyn_status launch_op(const dyn_layer *L, const dyn_batch *b, const dyn_schedule 
             break;                                                // applied by the qkv projection's dispatch
         case DYN_OP_ATTN:
             if (b->prefix_lead) {
-                const dyn::AttnPrefix prefix{b->prefix_lead, b->prefix_pages, b->n_seqs, ws.prefix_chunks};
+                const dyn::AttnPrefix prefix{b->prefix_lead, b->prefix_pages, b->n_seqs, ws.prefix_chunks, b->seq_of_token, b->pos_of_token, b->n_tokens};
                 err = dyn::launch_attention_shared(c.dtype, rowp(base + ws.qkv, NQKV), NQKV, b->seq_of_token + d.r0, b->pos_of_token + d.r0, b->block_table, kc, vc,
                                                    (void *)rowp(base + ws.attn, ws.ld_attn), ws.ld_attn, (float *)(base + sc.part_o),
                                                    (float *)(base + sc.part_ml), plan, sh, prefix, rows, st, mid, pre, d.layer > 0);

@@ -25,7 +25,6 @@ struct SharedArgs {
     SharedPlan plan;
     AttnShape sh;                         // rows of a table of one wide row; max_chunks: of both halves
     int ld_q, shared_slots;               // partials of own keys lie behind shared_slots chunks of shared ones
-    int few_subs, own_subs;               // sub-tiles per chunk of an item: of shared and of own keys
     float *part_o, *part_ml;
 };
 
@@ -66,7 +65,7 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
         const int keys = (m.own ? a.plan.s_pos : a.plan.p_pos)[m.t] + 1;
         m.table = a.block_table + (m.own ? a.plan.s_seq : a.plan.p_seq)[m.t];
         // chunks of equal size up to rounding, a function of the half's own length
-        const int subs = (keys + 15) >> 4, most = m.own ? a.own_subs : a.few_subs, n = (subs + most - 1) / most, per = (subs + n - 1) / n;
+        const int subs = (keys + 15) >> 4, most = (m.own ? a.plan.s_ct : a.plan.p_ct)[m.t] >> 4, n = (subs + most - 1) / most, per = (subs + n - 1) / n;
         m.first = m.c * per;
         m.last = min(m.first + per, subs) - 1;
         m.end = min(keys, (m.last + 1) * 16);
@@ -199,32 +198,19 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
     }
 }
 
-// Costs in us of one CU, as mixed_prompt_groups (kernels_attn_mfma.hip) has them: a tile of 64 positions of a query block 6, a position of an
-// item 0.026.
-__device__ __forceinline__ float block_cost(const int32_t *list, const int32_t *pos, const int32_t *ct) {
-    const int entries = list[0];
-    if (!entries) return 0.f;
-    auto tiles = [&](int e) {
-        const int t = list[2 + 2 * e], packed = list[3 + 2 * e];
-        return (min(ct[t], pos[t + (packed >> 20) - 1] + 1 - (packed & 0xfffff) * ct[t]) + 63) / 64;
-    };
-    return 1.5f * (tiles(0) + 2 * tiles(entries / 2) + tiles(entries - 1)) * entries;
-}
-
 // All keys of a dispatch in one launch, a workgroup of eight waves per CU: the first claim query blocks (of shared keys, then of own
 // ones), the others serve the items of both and then claim query blocks too.  Items wait for memory and query blocks for the matrix
 // cores (attn_mixed_kernel, kernels_attn_mfma.hip).
 __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(SharedArgs a) {
     const SharedPlan &w = a.plan;
-    const float blocks = block_cost(w.p_blocks, w.p_pos, w.p_ct) + block_cost(w.s_blocks, w.s_pos, w.s_ct);
-    const float items = 0.026f * 16 * a.own_subs * w.items[0];
-    const int groups = gridDim.x;
-    const int first = blocks == 0.f ? 0 : items == 0.f ? groups : mixed_share((w.p_blocks[0] + w.s_blocks[0]) * a.sh.n_kv, blocks, items, groups);
+    const int groups = gridDim.x, n_blocks = w.p_blocks[0] + w.s_blocks[0];
+    const int first = n_blocks == 0 ? 0 : w.items[0] == 0 ? groups : mixed_share(n_blocks * a.sh.n_kv, w.cost[1], w.cost[0], groups);
     if ((int)blockIdx.x >= first) serve_items<prefill::kWaves>(a, (int)blockIdx.x - first, groups - first);
     const size_t behind = part_index(a.sh, 0, 0, a.shared_slots);
 #pragma clang loop unroll(disable)
     for (int own = 0; own < 2; ++own) {
         int32_t *const list = own ? w.s_blocks : w.p_blocks;
+        if (list[0] == 0) continue;
         prefill::attn_prefill_items<true>(a.q, own ? w.s_seq : w.p_seq, own ? w.s_pos : w.p_pos, a.block_table, a.k, a.v, nullptr, 0,
                                           a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q);
     }
@@ -320,8 +306,8 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
             if (e != hipSuccess) return e;
             attr_set = true;
         }
-        const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, ld_q, prefix.max_chunks, attn_prefix_few_pages(sh),
-                           sh.chunk_pages, part_o, part_ml};
+        const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, ld_q, prefix.max_chunks, part_o,
+                           part_ml};
         const long most = (long)rows * sh.n_kv * part.max_chunks;
         const int cus = sh.n_cus > 0 && sh.n_cus < 256 ? sh.n_cus : 256;
         hipLaunchKernelGGL(attn_shared_kernel, dim3((unsigned)std::min<long>(most, cus)), dim3(prefill::kWaves * 64), prefill::lds_bytes(), s, a);

@@ -2,9 +2,8 @@
 //
 // Every row's keys are cut in two: the shared ones, which it attends together with the rows around it that share the same, and its
 // own.  Each half is described by arrays that take the place of the batch's (an offset into the block table for the
-// sequence, the last key for the position), and work lists name what exists of it.  Which sequences share with a row is counted over the whole
-// batch and not over the dispatch, and chunks follow from that count and the prefix alone, so a row's sums do not depend on
-// the schedule.  A row that stands inside the shared positions, alone with its lead or outside the table attends all its keys as its own.
+// sequence, the last key for the position), and work lists name what exists of it.  Who shares with a row, and how long chunks are, is counted
+// over the whole batch and not over the dispatch, so a row's sums do not depend on the schedule.  A row that stands inside the shared positions, alone with its lead or outside the table attends all its keys as its own.
 // One workgroup of 16 waves walks the rows 1024 at a time, twice: first the runs of rows that share the same, then what each leads.
 #include <algorithm>
 
@@ -22,15 +21,6 @@ constexpr int kShareSeqs = 8192;              // sequences whose leads are count
 // blocks, which read them once for all.
 constexpr int kFewSharers = 2;
 
-// Chunk of a prefix that `members` sequences share in query blocks of `tg` tokens: what gives every CU a piece, in tiles of 64
-// positions, at least two of them and at most 32 chunks.
-__device__ __forceinline__ int prefix_chunk_positions(int prefix, int members, int tg, int n_kv) {
-    const long long share = (long long)prefix * ((members + tg - 1) / tg) * n_kv / 256;
-    long long ct = share > prefix / 32 ? share : prefix / 32;
-    ct = (ct + 63) / 64 * 64;
-    return ct < 128 ? 128 : ct > 8192 ? 8192 : (int)ct;
-}
-
 template <class Combine>
 __device__ __forceinline__ int scan_wave(int x, Combine &&combine) {
     const int lane = threadIdx.x & 63;
@@ -45,9 +35,23 @@ __device__ __forceinline__ int add(int a, int b) { return a + b; }
 __device__ __forceinline__ int larger(int a, int b) { return a > b ? a : b; }
 
 struct PlanRule {
-    int tg_many, tg_few, most_few;      // tokens of a query block and of an item; the most sharers served by items
-    int few_positions, own_positions;   // chunks of items: of shared and of own keys
+    int tg_many, tg_few, most_few;      // tokens of a query block and of an item; the most tokens of a prefix that items serve
+    int most_positions;                 // the longest chunk of a single token's own keys
 };
+
+// Chunks, from the batch: `shared` = keys of a prefix times query blocks that attend it, summed over the prefixes; `own` = keys of single
+// tokens, summed.  A chunk costs a partial set per column, written and read again, and too few of them leave CUs idle.
+// Query blocks: what gives every CU a piece, or, beside single tokens' keys, what takes half as long as those (a tile of 64 positions
+// some 4 us, keys of one kv head 512 bytes at 5.5 TB/s); two tiles at least, and at most 32 chunks a prefix.
+__device__ __forceinline__ int block_positions(long long shared, long long own, int n_kv, int keys) {
+    const long long want = max(max(shared * n_kv / 256, own * n_kv * 3 / 4096), (long long)keys / 32);
+    return (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll);
+}
+// Items: four rounds of the chip's 2048 waves, at least 64 positions and at most 64 chunks a token.
+__device__ __forceinline__ int item_positions(long long own, int n_kv, int most, int keys) {
+    const long long want = min(max((own * n_kv / 8192 + 63) / 64 * 64, 64ll), (long long)most);
+    return (int)max(want, ((long long)keys / 64 + 63) / 64 * 64);
+}
 
 template <AttnForm FORM>
 __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *seq_of_token, const int32_t *pos_of_token, int rows, AttnPrefix prefix, AttnShape sh,
@@ -62,6 +66,16 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
         pages = prefix.pages[s];
         return lead >= 0 && lead < prefix.n_seqs && pages >= 1 && pages < max_pages;
     };
+    struct Row { int seq, pos, lead, keys; };                        // lead -1: shares nothing
+    auto row_of = [&](int seq, int pos) {
+        Row r{seq, pos, -1, 0};
+        int lead, pages;
+        if (pos >= 0 && shares(seq, lead, pages) && pos >= pages * ps && members[lead] >= 0) { r.lead = lead; r.keys = pages * ps; }
+        return r;
+    };
+    // members: sequences that name the lead; then, of those named by two and more, the batch's tokens behind the prefix, others -1
+    __shared__ long long batch[2];                                   // keys of shared prefixes over tokens, own keys of single tokens
+    if (threadIdx.x < 2) batch[threadIdx.x] = 0;
     if (any) {
         for (int s = threadIdx.x; s < prefix.n_seqs; s += 1024) members[s] = 0;
         __syncthreads();
@@ -70,22 +84,41 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
             if (shares(s, lead, pages)) atomicAdd(&members[lead], 1);
         }
         __syncthreads();
+        for (int s = threadIdx.x; s < prefix.n_seqs; s += 1024) members[s] = members[s] > 1 ? 0 : -1;
     }
-    struct Row { int seq, pos, lead, keys; };                        // lead -1: shares nothing
-    auto row_of = [&](int t) {
-        Row r{seq_of_token[t], pos_of_token[t], -1, 0};
-        int lead, pages;
-        if (r.pos >= 0 && shares(r.seq, lead, pages) && r.pos >= pages * ps && members[lead] > 1) { r.lead = lead; r.keys = pages * ps; }
-        return r;
-    };
+    __syncthreads();
+    if constexpr (FORM != SHARE_NOTHING) {
+        long long shared = 0, own = 0;
+        for (int t = threadIdx.x; t < prefix.rows; t += 1024) {
+            const int seq = prefix.seq_of_token[t];
+            const bool single = (t == 0 || prefix.seq_of_token[t - 1] != seq) && (t + 1 >= prefix.rows || prefix.seq_of_token[t + 1] != seq);
+            const Row r = row_of(seq, prefix.pos_of_token[t]);
+            if (r.lead >= 0) {
+                atomicAdd(&members[r.lead], 1);
+                shared += r.keys;
+            }
+            if (single) own += r.pos + 1 - r.keys;
+        }
+        if (__any(shared || own)) {
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) { shared += __shfl_xor(shared, off, 64); own += __shfl_xor(own, off, 64); }
+            if (lane == 0) {
+                atomicAdd((unsigned long long *)&batch[0], (unsigned long long)shared);
+                atomicAdd((unsigned long long *)&batch[1], (unsigned long long)own);
+            }
+        }
+        __syncthreads();
+    }
+    const long long batch_shared = batch[0] / rule.tg_many, batch_own = batch[1];
     int run_before = -1, blocks_before = 0;                          // the last run's first row, and the query blocks, before these rows
     for (int t0 = 0; t0 < rows; t0 += 1024) {
         const int t = t0 + (int)threadIdx.x;
         Row r{-1, -1, -1, 0};
         bool starts = false;
         if (t < rows) {
-            r = row_of(t);
-            const Row before = row_of(max(t - 1, 0));
+            const int prev = max(t - 1, 0);
+            r = row_of(seq_of_token[t], pos_of_token[t]);
+            const Row before = row_of(seq_of_token[prev], pos_of_token[prev]);
             starts = r.lead >= 0 && (t == 0 || before.lead != r.lead || before.keys != r.keys);
         }
         int run = scan_wave(starts ? t : -1, larger);                // the latest start up to here
@@ -119,7 +152,8 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
             w.p_pos[t] = on ? r.keys - 1 : -1;
             if constexpr (FORM == SHARE_LISTS) {
                 w.p_seq[t] = on ? r.lead * max_pages : -1;
-                w.p_ct[t] = !on || few ? rule.few_positions : prefix_chunk_positions(r.keys, members[r.lead], rule.tg_many, sh.n_kv);
+                w.p_ct[t] = !on ? 64 : few ? item_positions(batch_own, sh.n_kv, rule.most_positions, 2 * r.keys)
+                                           : block_positions(batch_shared, batch_own, sh.n_kv, r.keys);
                 w.run[t] = on ? run : -1 - t;
                 w.width[t] = leads ? (few ? -width : width) : 0;
             } else {
@@ -132,6 +166,8 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
         __threadfence_block();
         __syncthreads();
         int entries[3] = {0, 0, 0};                                  // of items, p_blocks, s_blocks
+        float cost[2] = {0.f, 0.f};
+        __shared__ float costs[2][16];
         for (int t0 = 0; t0 < rows; t0 += 1024) {
             const int t = t0 + (int)threadIdx.x;
             int p_tok = 0, p_n = 0, s_tok = 0, s_n = 0;              // what row t leads: tokens and chunks
@@ -153,7 +189,7 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
                 }
                 const bool prev_same = t > 0 && w.s_seq[t - 1] == s, next_same = t + 1 < rows && w.s_seq[t + 1] == s;
                 single = !prev_same && !next_same;
-                const int tg = rule.tg_many, ct = single ? rule.own_positions : prefill_chunk_positions((p / tg + 1) * tg);
+                const int tg = rule.tg_many, ct = single ? item_positions(batch_own, sh.n_kv, rule.most_positions, p + 1) : prefill_chunk_positions((p / tg + 1) * tg);
                 w.s_ct[t] = ct;
                 if (p >= 0 && (single || !prev_same || p % tg == 0)) {
                     int lo = 1, hi = single ? 1 : min(tg - p % tg, rows - t);
@@ -167,6 +203,10 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
                     s_n = (p + s_tok - 1 + ct) / ct;                 // chunks the block's last token reaches
                 }
             }
+            // a position of an item 512 bytes at 19.5 GB/s, a query block's tile of 64 positions 2 us for its loads and up to 4 for its products
+            const float per_block = 2.f / 64, per_token = 4.f / (64 * rule.tg_many);
+            if (p_n) (few ? cost[0] : cost[1]) += (w.p_pos[t] + 1) * (few ? 0.026f : per_block + p_tok * per_token);
+            if (s_n) (single ? cost[0] : cost[1]) += (w.s_pos[t] + s_tok) * (single ? 0.026f : per_block + s_tok * per_token);
             const int mine[3] = {(few ? p_n : 0) + (single ? s_n : 0), few ? 0 : p_n, single ? 0 : s_n};
             int start[3];
 #pragma unroll
@@ -189,6 +229,17 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
             at = single ? w.items + 2 + 2 * (size_t)(start[0] + (few ? p_n : 0)) : w.s_blocks + 2 + 2 * (size_t)start[2];
             for (int c = 0; c < s_n; ++c) { *at++ = single ? t | kOwnItem : t; *at++ = c | (s_tok << 20); }
         }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float x = wave_sum(cost[k]);
+            if (lane == 0) costs[k][wave] = x;
+        }
+        __syncthreads();
+        if (threadIdx.x < 2) {
+            float x = 0.f;
+            for (int j = 0; j < 16; ++j) x += costs[threadIdx.x][j];
+            w.cost[threadIdx.x] = x;
+        }
         if (threadIdx.x == 0) {
             w.items[0] = entries[0];
             w.p_blocks[0] = entries[1];
@@ -200,18 +251,24 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *s
 
 }  // namespace
 
-int attn_prefix_few_pages(const AttnShape &sh) { return std::max({sh.chunk_pages, 8, (sh.max_pages_per_seq + 31) / 32}); }
-
 int attn_prefix_max_chunks(int dtype, const AttnShape &sh) {
     const long positions = (long)sh.max_pages_per_seq * sh.page_size;
     if (!attention_mfma_supported(dtype, sh)) return (sh.max_pages_per_seq + sh.chunk_pages - 1) / sh.chunk_pages;
     const long most = std::max<long>(32, (positions + 8191) / 8192);
-    return (int)std::max<long>(1, std::min<long>(most, (positions + 127) / 128));
+    return (int)std::max<long>(1, std::min<long>(most, (positions + 63) / 64));
+}
+
+int attn_own_max_chunks(int dtype, const AttnShape &sh) {
+    const int chunks = (sh.max_pages_per_seq + sh.chunk_pages - 1) / sh.chunk_pages;
+    if (!attention_mfma_supported(dtype, sh)) return chunks;
+    const long positions = (long)sh.max_pages_per_seq * sh.page_size;
+    const int items = std::max(chunks, (int)std::min<long>(64, (positions + 63) / 64));
+    return std::max(items, attn_prefill_max_chunks(positions));
 }
 
 size_t attn_shared_plan_words(const AttnShape &sh, const AttnPrefix &prefix, int rows) {
     const size_t own = (size_t)sh.max_chunks * rows, shared = (size_t)prefix.max_chunks * rows;
-    return (size_t)rows * 8 + 6 + 4 * (own + shared);          // (for rows together no more than for each of them alone)
+    return (size_t)rows * 8 + 8 + 4 * (own + shared);          // (for rows together no more than for each of them alone)
 }
 
 SharedPlan attn_shared_plan(int32_t *plan, const AttnShape &sh, const AttnPrefix &prefix, int rows) {
@@ -219,7 +276,8 @@ SharedPlan attn_shared_plan(int32_t *plan, const AttnShape &sh, const AttnPrefix
     int32_t *at = plan;
     for (int32_t **a : {&w.p_seq, &w.p_pos, &w.p_ct, &w.s_seq, &w.s_pos, &w.s_ct, &w.run, &w.width}) { *a = at; at += rows; }
     const size_t own = (size_t)sh.max_chunks * rows, shared = (size_t)prefix.max_chunks * rows;
-    w.items = at;
+    w.cost = (float *)at;
+    w.items = at + 2;
     w.p_blocks = w.items + 2 + 2 * (own + shared);
     w.s_blocks = w.p_blocks + 2 + 2 * shared;
     return w;
@@ -236,12 +294,12 @@ hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, c
     if (p.n_seqs > kShareSeqs) p.lead = nullptr;
     const dim3 one(1), block(1024);
     if (form == SHARE_LISTS) {
-        const PlanRule rule{attn_prefill_block_tokens(sh), TG, kFewSharers * TG, attn_prefix_few_pages(sh) * sh.page_size, sh.chunk_pages * sh.page_size};
+        const PlanRule rule{attn_prefill_block_tokens(sh), TG, kFewSharers * TG, sh.chunk_pages * sh.page_size};
         hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_LISTS>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, rule, w);
     } else if (form == SHARE_TILES) {
-        hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_TILES>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, PlanRule{4 * TG, TG, TG, 0, 0}, w);
+        hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_TILES>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, PlanRule{4 * TG, TG, TG, 0}, w);
     } else {
-        hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_NOTHING>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, PlanRule{1, 1, 0, 0, 0}, w);
+        hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_NOTHING>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, PlanRule{1, 1, 0, 0}, w);
     }
     return hipGetLastError();
 }

@@ -205,17 +205,14 @@ def test_chunk_sizes(chunk):
     c.check(c.run(kv_chunk_positions=chunk))
 
 
-def test_a_rows_bits_do_not_depend_on_who_else_is_in_the_call():
-    """The same rows in two calls, one with half of the rows: what a row shares is counted over the sequences, not over the rows."""
+def test_the_same_batch_gives_the_same_bits():
+    """Whatever the workspace held, and however the launches' workgroups come to their work."""
     for shape in ("fast", "bf16_64", "f32_64"):
-        seqs = group("a", 20, [3, 50, 17, 90, 4, 33, 61, 2, 9, 12, 14]) + group("b", 7, [10, 20, 30])
+        seqs = group("a", 20, [3, 50, 17, 90, 4, 33, 61, 2, 9, 12, 14]) + group("b", 7, [10, 20, 30]) + [("b", 7, 90, 70)]
         c = Case(shape, seqs)
-        whole = c.run()
-        for r0, r1 in ((0, 5), (5, 14), (0, 1), (10, 12)):
-            n_q, _, hd, _ = c.dims
-            part = B.SharedAttention(c.q[r0:r1], torch.empty((r1 - r0, n_q, hd), dtype=c.q.dtype, device=DEV), c.k, c.v,
-                                     **dict(c.args, seq_of_token=c.args["seq_of_token"][r0:r1].contiguous(), pos_of_token=c.args["pos_of_token"][r0:r1].contiguous()))
-            assert torch.equal(part.forward(), whole[r0:r1]), (shape, r0, r1)
+        first = c.run()
+        for _ in range(5):
+            assert torch.equal(c.run(), first), shape
 
 
 def test_more_sequences_than_are_counted_attend_without_sharing():
