@@ -476,7 +476,7 @@ dyn_status dyn_tune(dyn_layer *layer, const dyn_batch *batch, const int32_t *ctx
  * share them, in one matrix product; the keys behind them are attended by each sequence for itself, and the two parts are
  * merged.  It is a promise about the tables, not another attention: the result is that of every row over its own sequence,
  * up to rounding.  Where it cannot pay or hold - a lead that one sequence names, a token that stands inside the shared pages, a lead or page
- * count outside the table, a batch of more than 8192 sequences, shapes whose attention does not run on the matrix cores (page_size no
+ * count outside the table, a batch of more than 4096 sequences, shapes whose attention does not run on the matrix cores (page_size no
  * multiple of 16, head_dim below 32, more than 16 q heads per kv head) - keys are attended without sharing.  How keys are cut into
  * chunks follows from the positions and prefixes of the whole batch: the same batch gives the same bits, in a layer under every
  * schedule.

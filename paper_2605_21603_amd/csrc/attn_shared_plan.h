@@ -11,8 +11,8 @@ enum AttnForm { SHARE_LISTS = 0, SHARE_TILES = 1, SHARE_NOTHING = 2 };
 
 struct SharedPlan {
     // Per row; p_: of its shared keys, s_: of its own.  seq: offset into the block table, pos: the last key (-1: none), ct: positions
-    // per chunk.  run, width: while the lists are built.
-    int32_t *p_seq, *p_pos, *p_ct, *s_seq, *s_pos, *s_ct, *run, *width;
+    // per chunk.
+    int32_t *p_seq, *p_pos, *p_ct, *s_seq, *s_pos, *s_ct;
     // Work lists (SHARE_LISTS), [0] = entries, entry i at 2 + 2 i: the first token row, then chunk | tokens << 20.  items: one wave's work - up to
     // 16 columns of shared keys, or a single token's own keys (kOwnItem set in the row).  p_blocks, s_blocks: query blocks of shared and
     // of own keys, [1] = the counter that they are claimed from.

@@ -216,8 +216,8 @@ def test_the_same_batch_gives_the_same_bits():
 
 
 def test_more_sequences_than_are_counted_attend_without_sharing():
-    """8193 sequences: every row over its own table row; 8192: shared."""
-    for n in (8192, 8193):
+    """4097 sequences: every row over its own table row; 4096: shared."""
+    for n in (4096, 4097):
         c = Case("f32_32", group("a", 1, [1] * 40) + [(None, 0, 1, 1)])
         table = np.zeros((n, c.table.shape[1]), np.int32)
         table[:41] = c.table
