@@ -216,60 +216,69 @@ __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(Sh
     }
 }
 
-// Merge of a row's partials, shared chunks first, in order: a half-wave per (token, q head), four head-dim indices to a lane (two sets of
-// them beyond 128).  A row without keys is zero.  ct null: chunks of `chunk` positions.
-template <typename T, bool BASE2>
+// Merge of a row's partials, shared chunks first, in order: a half-wave per (token, q head), four head-dim indices to a lane, two
+// sets of them in the WIDE form (head dims above 128).  A row without keys is zero.  ct null: chunks of `chunk` positions.  What it costs is two
+// dependent loads, of the row's chunk counts and of its partials, so the first kMergeLoads of those are on their way beside the maxima and sums
+// that weigh them.
+constexpr int kMergeLoads = 16;
+template <typename T, bool BASE2, bool WIDE>
 __global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
                                                                   const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
                                                                   const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct, int chunk,
                                                                   int shared_slots, T *__restrict__ out, int ld_out, AttnShape sh,
                                                                   int32_t *__restrict__ counter0, int32_t *__restrict__ counter1) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    constexpr int SETS = WIDE ? 2 : 1, LOADS = kMergeLoads / SETS;
     // the lists' query blocks have all been claimed: from the start again for the next layer
     if (counter0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) *(threadIdx.x ? counter1 : counter0) = 0;
     const int t = blockIdx.x, sub = threadIdx.x & 31, h = blockIdx.y * 8 + (threadIdx.x >> 5), d = sh.head_dim;
     if (h >= sh.n_q) return;
-    const int pc = p_ct ? p_ct[t] : chunk, sc = s_ct ? s_ct[t] : chunk;
-    const int n_shared = p_pos[t] < 0 ? 0 : (p_pos[t] + pc) / pc, n_own = s_pos[t] < 0 ? 0 : (s_pos[t] + sc) / sc, n = n_shared + n_own;
+    const int pp = p_pos[t], sp = s_pos[t], pc = p_ct ? p_ct[t] : chunk, sc = s_ct ? s_ct[t] : chunk;
+    const int n_shared = pp < 0 ? 0 : (pp + pc) / pc, n_own = sp < 0 ? 0 : (sp + sc) / sc, n = n_shared + n_own;
     T *const y = out + (size_t)t * ld_out + h * d;
-    auto at = [&](int c) { return part_index(sh, t, h, c < n_shared ? c : shared_slots + c - n_shared); };
-    float M = -INFINITY;
-    for (int c = sub; c < n; c += 32) M = fmaxf(M, part_ml[at(c) * 2]);
+    f32x4 acc[SETS];
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 32));
-    float L = 0.f;
-    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-    for (int cb = 0; cb < n; cb += 32) {
-        const int c = cb + sub;
-        float wgt = 0.f, wl = 0.f;
-        if (c < n) {
-            const float dm = part_ml[at(c) * 2] - M;
-            wgt = BASE2 ? exp2f(dm) : expf(dm);
-            wl = wgt * part_ml[at(c) * 2 + 1];
-        }
+    for (int k = 0; k < SETS; ++k) acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float inv = 0.f;
+    if (n) {
+        const size_t first = part_index(sh, t, h, 0), next = sh.n_q;                         // from a chunk to the one behind it
+        auto at = [&](int c) { return first + (size_t)(c < n_shared ? c : shared_slots + c - n_shared) * next; };
+        auto ml_of = [&](int c) { return c < n ? *reinterpret_cast<const f32x2 *>(part_ml + at(c) * 2) : f32x2{-INFINITY, 0.f}; };
+        f32x4 v[LOADS][SETS];
+        auto load = [&](int c0) {
 #pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) wl += __shfl_xor(wl, off, 32);
-        L += wl;
-        const int nb = min(32, n - cb);
-        for (int j0 = 0; j0 < nb; j0 += 8) {
-            f32x4 v[8][2];
+            for (int j = 0; j < LOADS; ++j)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+                for (int k = 0; k < SETS; ++k)
+                    v[j][k] = *reinterpret_cast<const f32x4 *>(part_o + at(min(c0 + j, n - 1)) * d + min(sub * 4 + k * 128, d - 4));
+        };
+        f32x2 ml = ml_of(sub);
+        load(0);
+        float M = ml[0];
+        for (int c = sub + 32; c < n; c += 32) M = fmaxf(M, ml_of(c)[0]);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int i = sub * 4 + k * 128;
-                    v[j][k] = (j0 + j < nb && i < d) ? *reinterpret_cast<const f32x4 *>(part_o + at(cb + j0 + j) * d + i) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 32));
+        float L = 0.f;
+        for (int cb = 0; cb < n; cb += 32) {
+            if (cb) ml = ml_of(cb + sub);
+            const float dm = ml[0] - M, wgt = BASE2 ? exp2f(dm) : expf(dm);                  // 0 past the last chunk
+            L += wgt * ml[1];
+            for (int j0 = 0; j0 < 32 && cb + j0 < n; j0 += LOADS) {
+                if (cb + j0) load(cb + j0);
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) {
+                    const float wj = __shfl(wgt, j0 + j, 32);
+#pragma unroll
+                    for (int k = 0; k < SETS; ++k) acc[k] += v[j][k] * wj;
                 }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float wj = __shfl(wgt, j0 + j, 32);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) acc[k] += v[j][k] * wj;
             }
         }
-    }
-    const float inv = n ? 1.0f / L : 0.f;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+        for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor(L, off, 32);
+        inv = 1.0f / L;
+    }
+#pragma unroll
+    for (int k = 0; k < SETS; ++k) {
         const int i = sub * 4 + k * 128;
         if (i < d) {
             if constexpr (sizeof(T) == 2) {
@@ -323,14 +332,20 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
     if (e != hipSuccess) return e;
     const bool lists = form == SHARE_LISTS;
     const dim3 grid(rows, (sh.n_q + 7) / 8), block(256);
-#define DYN_COMBINE(T, B2)                                                                                                                                     \
-    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2>), grid, block, 0, s, part_o, part_ml, w.p_pos, lists ? w.p_ct : nullptr, w.s_pos,                    \
-                       lists ? w.s_ct : nullptr, sh.chunk_pages * sh.page_size, prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr,  \
+#define DYN_COMBINE_AS(T, B2, WIDE)                                                                                                                         \
+    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE>), grid, block, 0, s, part_o, part_ml, w.p_pos, lists ? w.p_ct : nullptr, w.s_pos,             \
+                       lists ? w.s_ct : nullptr, sh.chunk_pages * sh.page_size, prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, \
                        lists ? w.s_blocks + 1 : nullptr)
+#define DYN_COMBINE(T, B2)                                      \
+    do {                                                        \
+        if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true);     \
+        else DYN_COMBINE_AS(T, B2, false);                      \
+    } while (0)
     if (dtype == 0) DYN_COMBINE(float, false);
     else if (form != SHARE_NOTHING) DYN_COMBINE(bf16_t, true);
     else DYN_COMBINE(bf16_t, false);
 #undef DYN_COMBINE
+#undef DYN_COMBINE_AS
     return hipGetLastError();
 }
 
