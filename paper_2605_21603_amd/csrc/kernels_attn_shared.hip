@@ -35,24 +35,27 @@ struct Item {
     const int32_t *table;
 };
 
-// The items, dealt to n_blocks workgroups of WAVES waves.  K and V go from memory straight into MFMA operand layout,
+// The items: every n_blocks-th from `block` on is this workgroup's, and its waves take them as they come, from a counter in LDS.  (A fixed share
+// to every wave: of the two waves of a SIMD the older gets its loads first, and with equal shares - 256 tokens of 1024 keys - the older ones were through
+// after 149 us and the others after 196.)  K and V go from memory straight into MFMA operand layout,
 //     S[16 pos, 16 cols]  = K_sub[16, 128] Q^T[128, 16]       (4 x mfma 16x16x32 per sub-tile)
 //     O^T[128, 16 cols]  += V^T[128, 32] P[32, 16]            (8 x mfma 16x16x32 per pair of sub-tiles)
 // with the D layout of the first product (lane: column l % 16, positions 4 (l / 16) + r) the B layout of the second.  Two register
 // buffers of 32 positions; the last pair of a chunk is followed by the first of the wave's next item, whose indices were
 // fetched while this one was multiplied.
-template <int WAVES>
-__device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int n_blocks) {
-    const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int n_blocks, int *taken) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
     const AttnShape &sh = a.sh;
-    const int n_items = a.plan.items[0] * sh.n_kv, n_waves = n_blocks * WAVES;
+    const int n_items = a.plan.items[0] * sh.n_kv;
     const int G = sh.n_q / sh.n_kv, col_tok = lr / G, col_head = lr - col_tok * G;
     const float scale = 1.4426950408889634f / sqrtf((float)HD);        // log2(e) / sqrt(d)
-    // few rounds: a wave of every workgroup first (what a CU gets from memory is bounded per CU)
-    const int gw = n_items < 4 * n_waves ? wave * n_blocks + block : block * WAVES + wave;
-    int round = 0;
-    auto item_at = [&](int k) { return k * n_waves + ((k & 1) ? n_waves - 1 - gw : gw); };
-    if (item_at(0) >= n_items) return;
+    auto take = [&]() {
+        int k = 0;
+        if (lane == 0) k = atomicAdd(taken, 1);
+        return block + __builtin_amdgcn_readfirstlane(k) * n_blocks;
+    };
+    int item = take();
+    if (item >= n_items) return;
 
     auto fetch = [&](int i) {
         Item m;
@@ -155,12 +158,13 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
     };
     const std::integral_constant<int, 0> b0;
     const std::integral_constant<int, 1> b1;
-    Item cur = fetch(item_at(0));
+    Item cur = fetch(item);
     load_q(q, cur);
     load(b0, cur, 0);
     while (true) {
-        const bool more = item_at(round + 1) < n_items;
-        const Item nxt = fetch(item_at(more ? round + 1 : round));       // the last one "prefetches" itself: harmless loads, no branch
+        const int next = take();
+        const bool more = next < n_items;
+        const Item nxt = fetch(more ? next : item);       // the last one "prefetches" itself: harmless loads, no branch
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         m_run = -INFINITY;
@@ -191,7 +195,7 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
             }
         }
         if (!more) break;
-        ++round;
+        item = next;
         cur = nxt;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) q[ks] = q_next[ks];
@@ -203,9 +207,12 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
 // cores (attn_mixed_kernel, kernels_attn_mfma.hip).
 __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(SharedArgs a) {
     const SharedPlan &w = a.plan;
+    __shared__ int taken;
+    if (threadIdx.x == 0) taken = 0;
+    __syncthreads();
     const int groups = gridDim.x, n_blocks = w.p_blocks[0] + w.s_blocks[0];
     const int first = n_blocks == 0 ? 0 : w.items[0] == 0 ? groups : mixed_share(n_blocks * a.sh.n_kv, w.cost[1], w.cost[0], groups);
-    if ((int)blockIdx.x >= first) serve_items<prefill::kWaves>(a, (int)blockIdx.x - first, groups - first);
+    if ((int)blockIdx.x >= first) serve_items(a, (int)blockIdx.x - first, groups - first, &taken);
     const size_t behind = part_index(a.sh, 0, 0, a.shared_slots);
 #pragma clang loop unroll(disable)
     for (int own = 0; own < 2; ++own) {

@@ -185,10 +185,11 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
                     s_n = (p + s_tok - 1 + s_ct) / s_ct;                                          // chunks the last of them reaches
                 }
             }
-            // a position of an item 512 bytes at 19.5 GB/s, a query block's tile of 64 positions 2 us for its loads and up to 4 for its products
+            // a position of an item 512 bytes at 19.5 GB/s; a query block's tile of 64 positions 1 us and up to 1 more where all its columns are live, a block and
+            // chunk 10 us around its tiles
             const int p_subs = p_n ? r.keys >> 4 : 0, s_subs = s_n ? (p + s_tok + 15) >> 4 : 0;
             cost_items += 7 * ((few ? p_subs : 0) + (single ? s_subs : 0));
-            cost_blocks += (few ? 0 : p_subs * 8 + p_subs * 16 / rule.tg_many * p_tok) + (single ? 0 : s_subs * 8 + s_subs * 16 / rule.tg_many * s_tok);
+            cost_blocks += (few ? 0 : p_subs * 4 + p_subs * 4 / rule.tg_many * p_tok + p_n * 160) + (single ? 0 : s_subs * 4 + s_subs * 4 / rule.tg_many * s_tok + s_n * 160);
         }
         const int mine[4] = {(few ? p_n : 0) + (single ? s_n : 0), few ? 0 : p_n, single ? 0 : s_n, leads};
         int start[4];
