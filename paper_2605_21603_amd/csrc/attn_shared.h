@@ -18,9 +18,6 @@ struct AttnPrefix {
     int rows = 0;
 };
 
-// Bits of a row's table offset in the general form's arrays (kernels_attn_generic.hip).
-constexpr int kTileSeq = (1 << 29) - 1, kTileWide = 1 << 29, kTileNarrow = 1 << 30;
-
 // The most chunks of a row's shared and of its own keys, of a batch whose rows have sh.max_pages_per_seq pages at most.
 int attn_prefix_max_chunks(int dtype, const AttnShape &sh);
 int attn_own_max_chunks(int dtype, const AttnShape &sh);

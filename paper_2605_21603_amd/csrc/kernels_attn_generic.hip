@@ -12,7 +12,7 @@
 // positions; attn_generic_kernel (one wave per (token, q head, chunk), plain loops) takes the rest.
 #include <algorithm>
 
-#include "attn_shared.h"
+#include "attn_shared_plan.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -86,7 +86,7 @@ struct TileList {
 #pragma unroll
         for (int i = 0; i < kRowsPerThread; ++i) {
             const bool ends = r0 + i + 1 >= rows || seq[i + 1] != seq[i] || quotient(pos[i + 1], rule.per_block) != quotient(pos[i], rule.per_block);
-            if (r0 + i < rows && ends && pos[i] >= 0) n += quotient(pos[i], rule.per_chunk) + 1;
+            if (r0 + i < rows && ends) n += quotient(pos[i], rule.per_chunk) + 1;
             upto[i] = n;
         }
         int incl = n;
@@ -124,12 +124,19 @@ struct TileList {
     }
 };
 
-// PARTS: every item leaves partials for a merge of its own (kernels_attn_shared.hip), q rows are ld_q apart, and the bits of a sequence number above kTileSeq say how its group is served: kTileWide as
-// several tokens, however many are left of it, kTileNarrow by quarters of the chunk, up to 16 columns of them; the sign only tells adjacent groups apart.
+// PARTS: a piece of an attention over shared prefixes (kernels_attn_shared.hip).  The item says everything about its tokens, it leaves partials for a
+// merge of its own, and q rows are ld_q apart.
+struct TilePart {
+    int t, n_tok, c, g;                // first token row, tokens, chunk, kv head
+    int keys, step;                    // keys of the last token; each token before it has `step` less
+    int chunk, table;                  // positions per chunk; offset of the sequence's row in the block table
+    bool quarters, own;                // the waves take a quarter of the chunk each, and up to 16 columns; whose keys
+};
 template <typename T, int HD, int TP, bool PARTS>
 __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32_t *__restrict__ block_table, const T *__restrict__ k_cache,
                                           const T *__restrict__ v_cache, T *__restrict__ out, int ld_out, float *__restrict__ part_o,
-                                          float *__restrict__ part_ml, const AttnShape &sh, const TileRule &rule, const TileItem &item,
+                                          float *__restrict__ part_ml, const AttnShape &sh, const TileRule &rule,
+                                          const typename std::conditional<PARTS, TilePart, TileItem>::type &item,
                                           float (*merge_o)[16][(HD < 128 ? HD : 128) + 4], float (*merge_ml)[16][2], int ld_q) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NK = F32 ? HD / 16 : HD / 32, ND = HD / 16;      // 16-byte K operands and 16-row V operands of a lane
@@ -140,19 +147,37 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
     const int g = item.g, c = item.c;
     const int G = rule.G, TG = rule.TG, tg = rule.block;           // tokens per set of columns, per group
     const int col_tok = (lr * rule.g_mul) >> 16, col_head = lr - col_tok * G;   // this lane's column: a token of the wave's set and a q head
-    const int s = item.seq, p_last = item.pos, row_seq = item.row_seq, row_pos = item.row_pos;
-    const unsigned long long alike = __ballot(lane < tg && lane <= item.t_last && row_seq == s && quotient(row_pos, rule.per_block) == quotient(p_last, rule.per_block));
-    const int n_tok = PARTS ? (~alike ? __ffsll(~alike) - 1 : 64) : __popcll(alike);          // (a run that others cut has rows like these farther back)
-    const int t = item.t_last - n_tok + 1, n_keys = p_last + 1;    // the group's first token; keys its last token attends
-    const int ps = sh.page_size, ct = rule.chunk, j0 = c * ct;
+    int t, n_tok, n_keys, ct, row_pos = 0;                         // the group's first token, tokens, keys its last token attends, positions per chunk
+    bool single;
+    const int32_t *bt;
+    if constexpr (PARTS) {
+        t = item.t;
+        n_tok = item.n_tok;
+        n_keys = item.keys;
+        ct = item.chunk;
+        single = item.quarters;
+        bt = block_table + item.table;
+    } else {
+        const int s = item.seq, p_last = item.pos, row_seq = item.row_seq;
+        row_pos = item.row_pos;
+        n_tok = __popcll(__ballot(lane < tg && lane <= item.t_last && row_seq == s && quotient(row_pos, rule.per_block) == quotient(p_last, rule.per_block)));
+        t = item.t_last - n_tok + 1;
+        n_keys = p_last + 1;
+        ct = rule.chunk;
+        single = n_tok == 1;
+        bt = block_table + (size_t)s * sh.max_pages_per_seq;
+    }
+    const int ps = sh.page_size, j0 = c * ct;
     const int j1 = min(j0 + ct, n_keys);
-    const bool single = PARTS && (s & (kTileWide | kTileNarrow)) ? (s & kTileNarrow) != 0 : n_tok == 1;
-    const int32_t *bt = block_table + (size_t)(PARTS ? s & kTileSeq : s) * sh.max_pages_per_seq;
     const float tiles_per_page = 16.0f / (float)ps;
+    auto pos_of = [&](int tok) {                                   // of token `tok` of the group (PARTS)
+        if constexpr (PARTS) return n_keys - 1 - item.step * (n_tok - 1 - min(tok, n_tok - 1));
+        else return 0;
+    };
 
     const int set0 = single ? 0 : wave * TG;                       // first token of the wave's columns
     const bool live = col_tok < TG && set0 + col_tok < n_tok;
-    const int col_pos = __shfl(row_pos, max(n_tok - 1 - set0 - min(col_tok, TG - 1), 0), 64);   // every lane takes part
+    const int col_pos = PARTS ? pos_of(set0 + min(col_tok, TG - 1)) : __shfl(row_pos, max(n_tok - 1 - set0 - min(col_tok, TG - 1), 0), 64);   // every lane takes part
     const int col_keys = live ? col_pos + 1 : 0;                   // keys the column attends
     u32x4 qf[NK];
     const T *qp = qkv + (size_t)(t + (live ? set0 + col_tok : 0)) * (PARTS ? ld_q : (sh.n_q + 2 * sh.n_kv) * HD) + (size_t)(g * G + (live ? col_head : 0)) * HD;
@@ -173,7 +198,8 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
         w0 = j0 + min(wave * per, n_tile) * 16 * TP;
         free_keys = w1 = min(j1, w0 + per * 16 * TP);
     } else {
-        const int last = __builtin_amdgcn_readlane(row_pos, n_tok - min(set0 + TG, n_tok)), first = __builtin_amdgcn_readlane(row_pos, max(n_tok - 1 - set0, 0));
+        const int last = PARTS ? pos_of(set0 + TG - 1) : __builtin_amdgcn_readlane(row_pos, n_tok - min(set0 + TG, n_tok));
+        const int first = PARTS ? pos_of(set0) : __builtin_amdgcn_readlane(row_pos, max(n_tok - 1 - set0, 0));
         w1 = set0 < n_tok ? min(j1, last + 1) : j0;
         free_keys = min(w1, first + 1);
     }
@@ -440,13 +466,13 @@ __device__ __forceinline__ void attn_tile(const T *__restrict__ qkv, const int32
 
 // LIST: the workgroups walk the items that exist, dealt in turn; else one workgroup per (chunk, kv head, token) of the
 // dense grid, of which only a group's last token and the chunks it reaches have work.
-template <typename T, int HD, int TP, bool LIST, bool PARTS>
+template <typename T, int HD, int TP, bool LIST>
 __global__ __launch_bounds__(256, HD * sizeof(T) <= 256 ? 2 : 1) void attn_tile_kernel(const T *__restrict__ qkv, const int32_t *__restrict__ seq_of_token,
                                                         const int32_t *__restrict__ pos_of_token,
                                                         const int32_t *__restrict__ block_table, const T *__restrict__ k_cache,
                                                         const T *__restrict__ v_cache, T *__restrict__ out, int ld_out,
                                                         float *__restrict__ part_o, float *__restrict__ part_ml, AttnShape sh,
-                                                        TileRule rule, int rows, int y0, int y1, int ld_q) {
+                                                        TileRule rule, int rows, int y0, int y1) {
     __shared__ float merge_o[4][16][(HD < 128 ? HD : 128) + 4];
     __shared__ float merge_ml[4][16][2];
     auto item_of = [&](int t_last, int c, int g) {
@@ -454,7 +480,7 @@ __global__ __launch_bounds__(256, HD * sizeof(T) <= 256 ? 2 : 1) void attn_tile_
         return TileItem{t_last, c, g, seq_of_token[t_last], pos_of_token[t_last], seq_of_token[row], pos_of_token[row]};
     };
     auto serve = [&](const TileItem &item) {
-        attn_tile<T, HD, TP, PARTS>(qkv, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rule, item, merge_o, merge_ml, ld_q);
+        attn_tile<T, HD, TP, false>(qkv, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rule, item, merge_o, merge_ml, 0);
     };
     if constexpr (LIST) {
         __shared__ int scratch[8];
@@ -492,6 +518,48 @@ __global__ __launch_bounds__(256, HD * sizeof(T) <= 256 ? 2 : 1) void attn_tile_
         if (after > t && s_after == item.seq && quotient(p_after, rule.per_block) == quotient(item.pos, rule.per_block)) return;   // not the last token of its group
         if (c * rule.chunk > item.pos) return;
         serve(item);
+    }
+}
+
+// The lists of an attention over shared prefixes, query blocks first: shared and own keys of all rows in one launch.
+template <typename T, int HD, int TP>
+__global__ __launch_bounds__(256, HD * sizeof(T) <= 256 ? 2 : 1) void attn_parts_kernel(const T *__restrict__ q, const int32_t *__restrict__ block_table,
+                                                        const T *__restrict__ k_cache, const T *__restrict__ v_cache, float *__restrict__ part_o,
+                                                        float *__restrict__ part_ml, AttnShape sh, TileRule rule, SharedPlan w, int shared_slots, int ld_q) {
+    __shared__ float merge_o[4][16][(HD < 128 ? HD : 128) + 4];
+    __shared__ float merge_ml[4][16][2];
+    const int n_p = w.p_blocks[0], n_s = w.s_blocks[0], n_items = (n_p + n_s + w.items[0]) * sh.n_kv;
+    const size_t behind = part_index(sh, 0, 0, shared_slots);
+    auto fetch = [&](int n) {
+        TilePart m;
+        const int e = quotient(n, rule.per_kv);
+        const int32_t *const list = e < n_p ? w.p_blocks + 2 * (size_t)e : e < n_p + n_s ? w.s_blocks + 2 * (size_t)(e - n_p) : w.items + 2 * (size_t)(e - n_p - n_s);
+        const int row = list[2], packed = list[3];
+        m.g = n - e * sh.n_kv;
+        m.quarters = e >= n_p + n_s;
+        m.t = row & (kOwnItem - 1);
+        m.own = m.quarters ? row >= kOwnItem : e >= n_p;
+        m.c = packed & 0xfffff;
+        m.n_tok = packed >> 20;
+        m.keys = (m.own ? w.s_pos : w.p_pos)[m.t + m.n_tok - 1] + 1;
+        m.chunk = (m.own ? w.s_ct : w.p_ct)[m.t];
+        m.table = (m.own ? w.s_seq : w.p_seq)[m.t];
+        m.step = m.own;
+        return m;
+    };
+    int n = blockIdx.x;
+    if (n >= n_items) return;
+    TilePart cur = fetch(n);
+    while (true) {
+        n += gridDim.x;
+        const bool more = n < n_items;
+        TilePart nxt = cur;
+        if (more) nxt = fetch(n);
+        attn_tile<T, HD, TP, true>(q, block_table, k_cache, v_cache, (T *)nullptr, 0, part_o + (cur.own ? behind * HD : 0), part_ml + (cur.own ? behind * 2 : 0), sh, rule, cur,
+                                   merge_o, merge_ml, ld_q);
+        if (!more) break;
+        __syncthreads();                                           // the merge arrays are free again
+        cur = nxt;
     }
 }
 
@@ -849,17 +917,21 @@ constexpr size_t kGeneralGrid = (size_t)1 << 25;       // of the general form
 constexpr size_t kListGrid = 512;
 
 
-template <typename T, int HD, int TP, bool PARTS>
+TileRule tile_rule(const AttnShape &sh) {
+    const int G = sh.n_q / sh.n_kv, block = 4 * (16 / G), chunk = sh.chunk_pages * sh.page_size;
+    return TileRule{1.0 / block, 1.0 / chunk, 1.0 / sh.n_kv, G, 16 / G, block, chunk, 65536 / G + 1};
+}
+
+template <typename T, int HD, int TP>
 void launch_attn_tile(hipStream_t s, const void *qkv, const int32_t *seq_of_token, const int32_t *pos_of_token,
                       const int32_t *block_table, const void *k_cache, const void *v_cache, void *out, int ld_out, float *part_o,
-                      float *part_ml, const AttnShape &sh, int rows, int ld_q) {
+                      float *part_ml, const AttnShape &sh, int rows) {
     const int n_y = sh.n_kv * sh.max_chunks;
     const size_t dense = (size_t)rows * n_y;
-    const int G = sh.n_q / sh.n_kv, block = 4 * (16 / G), chunk = sh.chunk_pages * sh.page_size;
-    const TileRule rule{1.0 / block, 1.0 / chunk, 1.0 / sh.n_kv, G, 16 / G, block, chunk, 65536 / G + 1};
+    const TileRule rule = tile_rule(sh);
 #define DYN_TILE_LAUNCH(LIST, GRID, Y0, Y1)                                                                                              \
-    hipLaunchKernelGGL((attn_tile_kernel<T, HD, TP, LIST, PARTS>), dim3(GRID), dim3(256), 0, s, (const T *)qkv, seq_of_token, pos_of_token,     \
-                       block_table, (const T *)k_cache, (const T *)v_cache, (T *)out, ld_out, part_o, part_ml, sh, rule, rows, Y0, Y1, ld_q)
+    hipLaunchKernelGGL((attn_tile_kernel<T, HD, TP, LIST>), dim3(GRID), dim3(256), 0, s, (const T *)qkv, seq_of_token, pos_of_token,     \
+                       block_table, (const T *)k_cache, (const T *)v_cache, (T *)out, ld_out, part_o, part_ml, sh, rule, rows, Y0, Y1)
     if (rows <= kListRows && dense > kListGrid) {
         DYN_TILE_LAUNCH(true, (unsigned)std::min<size_t>(dense, HD * sizeof(T) >= 256 ? 512 : 1024), 0, n_y);
         return;
@@ -870,6 +942,30 @@ void launch_attn_tile(hipStream_t s, const void *qkv, const int32_t *seq_of_toke
         DYN_TILE_LAUNCH(false, (unsigned)(((size_t)rows * (y1 - y0) + 7) / 8 * 8), y0, y1);               // whole eights of workgroups
     }
 #undef DYN_TILE_LAUNCH
+}
+
+template <typename T, int HD, int TP>
+void launch_attn_parts(hipStream_t s, const void *q, int ld_q, const int32_t *block_table, const void *k_cache, const void *v_cache, float *part_o, float *part_ml,
+                       const AttnShape &sh, const SharedPlan &w, int shared_slots, int rows) {
+    const size_t most = (size_t)rows * sh.n_kv * sh.max_chunks;
+    hipLaunchKernelGGL((attn_parts_kernel<T, HD, TP>), dim3((unsigned)std::min<size_t>(most, HD * sizeof(T) >= 256 ? 512 : 1024)), dim3(256), 0, s, (const T *)q, block_table,
+                       (const T *)k_cache, (const T *)v_cache, part_o, part_ml, sh, tile_rule(sh), w, shared_slots, ld_q);
+}
+
+// f(storage type, head dim, sub-tiles of 16 positions per tile): two where a lane's K and V operands of both fit beside the
+// accumulators twice over, else one.
+template <class F>
+void for_tile(int dtype, int head_dim, F &&f) {
+    auto of = [&](auto t) {
+        switch (head_dim) {
+            case 32: f(t, std::integral_constant<int, 32>(), std::integral_constant<int, 2>()); break;
+            case 64: f(t, std::integral_constant<int, 64>(), std::integral_constant<int, 2>()); break;
+            case 128: f(t, std::integral_constant<int, 128>(), std::integral_constant<int, 1>()); break;
+            default: f(t, std::integral_constant<int, 256>(), std::integral_constant<int, 1>()); break;
+        }
+    };
+    if (dtype == 0) of(float());
+    else of(bf16_t());
 }
 
 hipError_t launch_attn_general(int dtype, hipStream_t s, const void *qkv, const int32_t *seq_of_token, const int32_t *pos_of_token, const int32_t *block_table,
@@ -890,40 +986,20 @@ hipError_t launch_attn_general(int dtype, hipStream_t s, const void *qkv, const 
     return hipGetLastError();
 }
 
-template <bool PARTS>
-void launch_attn_tiles(int dtype, hipStream_t s, const void *qkv, const int32_t *seq_of_token, const int32_t *pos_of_token,
-                       const int32_t *block_table, const void *k_cache, const void *v_cache, void *out, int ld_out, float *part_o,
-                       float *part_ml, const AttnShape &sh, int rows, int ld_q) {
-    // positions per tile: two sub-tiles of 16 where a lane's K and V operands of both fit beside the
-    // accumulators twice over, else one
-#define DYN_TILE(T, HD, TP) launch_attn_tile<T, HD, TP, PARTS>(s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rows, ld_q)
-    if (dtype == 0) {
-        switch (sh.head_dim) {
-            case 32: DYN_TILE(float, 32, 2); break;
-            case 64: DYN_TILE(float, 64, 2); break;
-            case 128: DYN_TILE(float, 128, 1); break;
-            default: DYN_TILE(float, 256, 1); break;
-        }
-    } else {
-        switch (sh.head_dim) {
-            case 32: DYN_TILE(bf16_t, 32, 2); break;
-            case 64: DYN_TILE(bf16_t, 64, 2); break;
-            case 128: DYN_TILE(bf16_t, 128, 1); break;
-            default: DYN_TILE(bf16_t, 256, 1); break;
-        }
-    }
-#undef DYN_TILE
-}
 }  // namespace
 
-// Partials, and nothing but partials, of rows described by arrays of their own (kernels_attn_shared.hip).  tile: attn_tile_takes said so.
+bool attn_tile_shape(const AttnShape &sh) { return attn_tile_supported(sh, nullptr, nullptr); }
 bool attn_tile_takes(const AttnShape &sh, const void *k_cache, const void *v_cache) { return attn_tile_supported(sh, k_cache, v_cache); }
-hipError_t launch_attention_parts(int dtype, bool tile, const void *q, int ld_q, const int32_t *seq_of_token, const int32_t *pos_of_token, const int32_t *block_table,
-                                  const void *k_cache, const void *v_cache, float *part_o, float *part_ml, const AttnShape &sh, int rows, hipStream_t s) {
-    if (tile) {
-        launch_attn_tiles<true>(dtype, s, q, seq_of_token, pos_of_token, block_table, k_cache, v_cache, nullptr, 0, part_o, part_ml, sh, rows, ld_q);
-        return hipGetLastError();
-    }
+
+hipError_t launch_attention_parts(int dtype, const void *q, int ld_q, const int32_t *block_table, const void *k_cache, const void *v_cache, float *part_o, float *part_ml,
+                                  const AttnShape &sh, const SharedPlan &w, int shared_slots, int rows, hipStream_t s) {
+    for_tile(dtype, sh.head_dim, [&](auto t, auto hd, auto tp) {
+        launch_attn_parts<decltype(t), decltype(hd)::value, decltype(tp)::value>(s, q, ld_q, block_table, k_cache, v_cache, part_o, part_ml, sh, w, shared_slots, rows);
+    });
+    return hipGetLastError();
+}
+hipError_t launch_attention_own(int dtype, const void *q, int ld_q, const int32_t *seq_of_token, const int32_t *pos_of_token, const int32_t *block_table, const void *k_cache,
+                                const void *v_cache, float *part_o, float *part_ml, const AttnShape &sh, int rows, hipStream_t s) {
     return launch_attn_general(dtype, s, q, seq_of_token, pos_of_token, block_table, k_cache, v_cache, part_o, part_ml, sh, rows, ld_q);
 }
 
@@ -935,7 +1011,10 @@ hipError_t launch_attention_generic(int dtype, const void *qkv, const int32_t *s
     if (rows >= 1 << 24) return hipErrorInvalidConfiguration;
     const bool tile = attn_tile_supported(sh, k_cache, v_cache);
     if (tile) {
-        launch_attn_tiles<false>(dtype, s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, out, ld_out, part_o, part_ml, sh, rows, 0);
+        for_tile(dtype, sh.head_dim, [&](auto t, auto hd, auto tp) {
+            launch_attn_tile<decltype(t), decltype(hd)::value, decltype(tp)::value>(s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, out, ld_out, part_o,
+                                                                                    part_ml, sh, rows);
+        });
     } else {
         const hipError_t e = launch_attn_general(dtype, s, qkv, seq_of_token, pos_of_token, block_table, k_cache, v_cache, part_o, part_ml, sh, rows,
                                                  (sh.n_q + 2 * sh.n_kv) * sh.head_dim);

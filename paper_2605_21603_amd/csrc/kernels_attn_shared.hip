@@ -224,14 +224,14 @@ __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(Sh
 }
 
 // Merge of a row's partials, shared chunks first, in order: a half-wave per (token, q head), four head-dim indices to a lane, two
-// sets of them in the WIDE form (head dims above 128).  A row without keys is zero.  ct null: chunks of `chunk` positions.  What it costs is two
+// sets of them in the WIDE form (head dims above 128).  A row without keys is zero.  What it costs is two
 // dependent loads, of the row's chunk counts and of its partials, so the first kMergeLoads of those are on their way beside the maxima and sums
 // that weigh them.
 constexpr int kMergeLoads = 16;
 template <typename T, bool BASE2, bool WIDE>
 __global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
                                                                   const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
-                                                                  const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct, int chunk,
+                                                                  const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct,
                                                                   int shared_slots, T *__restrict__ out, int ld_out, AttnShape sh,
                                                                   int32_t *__restrict__ counter0, int32_t *__restrict__ counter1) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *_
     if (counter0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) *(threadIdx.x ? counter1 : counter0) = 0;
     const int t = blockIdx.x, sub = threadIdx.x & 31, h = blockIdx.y * 8 + (threadIdx.x >> 5), d = sh.head_dim;
     if (h >= sh.n_q) return;
-    const int pp = p_pos[t], sp = s_pos[t], pc = p_ct ? p_ct[t] : chunk, sc = s_ct ? s_ct[t] : chunk;
+    const int pp = p_pos[t], sp = s_pos[t], pc = p_ct[t], sc = s_ct[t];
     const int n_shared = pp < 0 ? 0 : (pp + pc) / pc, n_own = sp < 0 ? 0 : (sp + sc) / sc, n = n_shared + n_own;
     T *const y = out + (size_t)t * ld_out + h * d;
     f32x4 acc[SETS];
@@ -328,20 +328,19 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
         const int cus = sh.n_cus > 0 && sh.n_cus < 256 ? sh.n_cus : 256;
         hipLaunchKernelGGL(attn_shared_kernel, dim3((unsigned)std::min<long>(most, cus)), dim3(prefill::kWaves * 64), prefill::lds_bytes(), s, a);
         e = hipGetLastError();
+    } else if (form == SHARE_TILES) {
+        e = launch_attention_parts(dtype, q, ld_q, block_table, k_cache, v_cache, part_o, part_ml, part, w, prefix.max_chunks, rows, s);
     } else {
-        const bool tile = form == SHARE_TILES;
         const size_t behind = part_index(part, 0, 0, prefix.max_chunks);
-        e = launch_attention_parts(dtype, tile, q, ld_q, w.s_seq, w.s_pos, block_table, k_cache, v_cache, part_o + behind * sh.head_dim, part_ml + behind * 2, part, rows, s);
-        if (e == hipSuccess && tile && prefix.lead)
-            e = launch_attention_parts(dtype, tile, q, ld_q, w.p_seq, w.p_pos, block_table, k_cache, v_cache, part_o, part_ml, part, rows, s);
+        e = launch_attention_own(dtype, q, ld_q, w.s_seq, w.s_pos, block_table, k_cache, v_cache, part_o + behind * sh.head_dim, part_ml + behind * 2, part, rows, s);
     }
     if (e == hipSuccess && mid) e = hipEventRecord(mid, s);
     if (e != hipSuccess) return e;
     const bool lists = form == SHARE_LISTS;
     const dim3 grid(rows, (sh.n_q + 7) / 8), block(256);
 #define DYN_COMBINE_AS(T, B2, WIDE)                                                                                                                         \
-    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE>), grid, block, 0, s, part_o, part_ml, w.p_pos, lists ? w.p_ct : nullptr, w.s_pos,             \
-                       lists ? w.s_ct : nullptr, sh.chunk_pages * sh.page_size, prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, \
+    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,                       \
+                       prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, \
                        lists ? w.s_blocks + 1 : nullptr)
 #define DYN_COMBINE(T, B2)                                      \
     do {                                                        \

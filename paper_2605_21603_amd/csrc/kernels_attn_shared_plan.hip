@@ -40,20 +40,23 @@ __device__ __forceinline__ int sum_all(int x) { return __builtin_amdgcn_readlane
 struct PlanRule {
     int tg_many, tg_few, most_few;      // tokens of a query block and of an item; the most tokens of a prefix that items serve
     int most_positions;                 // the longest chunk of a single token's own keys
+    int n_kv;
+    bool tiles;                         // SHARE_TILES
 };
 
 // Chunks, from the batch, in sub-tiles of 16 positions: `shared` = keys of a prefix times query blocks that attend it, summed over the
 // prefixes; `own` = keys of single tokens, summed.  A chunk costs a partial set per column, written and read again, and too few of them
-// leave CUs idle.  Query blocks: what gives every CU a piece, or, beside single tokens' keys, what takes half as long as those (a
-// tile of 64 positions some 4 us, keys of one kv head 512 bytes at 5.5 TB/s); two tiles at least, and at most 32 chunks a prefix.
-__device__ __forceinline__ int block_positions(long long shared, long long own, int n_kv, int keys) {
-    const long long want = max(max(shared * n_kv / 16, own * n_kv * 3 / 256), (long long)keys / 32);
+// leave CUs idle.  Query blocks: what gives every CU (general form: one of four workgroups to a CU) a piece, or, beside single tokens' keys,
+// what takes half as long as those (a tile of 64 positions some 4 us, keys of one kv head 512 bytes at 5.5 TB/s); two tiles at least, and at most
+// 32 chunks a prefix.
+__device__ __forceinline__ int block_positions(const PlanRule &rule, long long shared, long long own, int keys) {
+    const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 16, own * rule.n_kv * 3 / 256), (long long)keys / 32);
     return (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll);
 }
-// Items: four rounds of the chip's 2048 waves, at least 64 positions and at most 64 chunks a token.
-__device__ __forceinline__ int item_positions(long long own, int n_kv, int most, int keys) {
-    const long long want = min(max((own * n_kv / 512 + 63) / 64 * 64, 64ll), (long long)most);
-    return (int)max(want, ((long long)keys / 64 + 63) / 64 * 64);
+// Items: four rounds of the chip's 2048 waves (general form: two of 1024 workgroups), at least 64 (128) positions and at most 64 chunks a token.
+__device__ __forceinline__ int item_positions(const PlanRule &rule, long long own, int keys) {
+    const long long want = own * rule.n_kv / (rule.tiles ? 128 : 512), least = rule.tiles ? 128 : 64;
+    return (int)max(min(max((want + 63) / 64 * 64, least), (long long)rule.most_positions), ((long long)keys / 64 + 63) / 64 * 64);
 }
 
 // Set bits from bit `at` on, as far as they follow one another.
@@ -70,10 +73,9 @@ __device__ __forceinline__ int ones_from(const unsigned long long *words, int at
 }
 
 // One workgroup of 16 waves, a thread per row and round of 1024 rows.
-template <AttnForm FORM>
+template <bool SHARE>
 __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *__restrict__ seq_of_token, const int32_t *__restrict__ pos_of_token, int rows,
                                                                 AttnPrefix prefix, AttnShape sh, PlanRule rule, SharedPlan w) {
-    constexpr bool SHARE = FORM != SHARE_NOTHING;
     __shared__ int lead_of[SHARE ? kShareSeqs : 1], pages_of[SHARE ? kShareSeqs : 1], members[SHARE ? kShareSeqs : 1];
     __shared__ int batch[2], cost[2];                                // sub-tiles of shared and of own keys; what the lists take, in 1/16 us
     __shared__ int edge_lead[17], edge_keys[17], edge_seq[17];       // the last row of each wave's 64, and of the round before
@@ -119,7 +121,8 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
                 atomicAdd(&members[r.lead], 1);
                 shared += r.keys >> 4;
             }
-            if ((t == 0 || before != seq) && (t + 1 == prefix.rows || after != seq)) own += (r.pos - r.keys + 16) >> 4;
+            const bool first = t == 0 || before != seq, last = t + 1 == prefix.rows || after != seq;
+            if (rule.tiles ? first || (r.pos - r.keys) % rule.tg_many == 0 : first && last) own += (r.pos - r.keys + 16) >> 4;
         }
         shared = sum_all(shared);
         own = sum_all(own);
@@ -130,7 +133,7 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
         __syncthreads();
     }
     const long long batch_shared = batch[0] / rule.tg_many, batch_own = batch[1];
-    int run_before = -1, before[4] = {0, 0, 0, 0};                   // the last run's first row; entries of items, p_blocks, s_blocks, and query blocks so far
+    int run_before = -1, before[3] = {0, 0, 0};                      // the last run's first row; entries of items, p_blocks, s_blocks so far
     int cost_items = 0, cost_blocks = 0;
     for (int t0 = 0; t0 < rows; t0 += 1024) {
         const int t = t0 + tid;
@@ -170,8 +173,8 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
         const bool leads = on && (t - run) % width == 0;
         int p_tok = 0, p_n = 0, p_ct = 64, s_tok = 0, s_n = 0, s_ct = 64;              // what row t leads: tokens and chunks
         bool single = false;
-        if constexpr (FORM == SHARE_LISTS) {
-            if (on) p_ct = few ? item_positions(batch_own, sh.n_kv, rule.most_positions, 2 * r.keys) : block_positions(batch_shared, batch_own, sh.n_kv, r.keys);
+        if constexpr (SHARE) {
+            if (on) p_ct = few ? item_positions(rule, batch_own, 2 * r.keys) : block_positions(rule, batch_shared, batch_own, r.keys);
             if (leads) {
                 p_tok = min(width, 1 + ones_from(p_goes_on, tid + 1));
                 p_n = (r.keys - 1 + p_ct) / p_ct;
@@ -179,7 +182,7 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
             if (live && r.pos >= 0) {
                 const int tg = rule.tg_many;
                 single = !same_seq && !(s_goes_on[(tid + 1) >> 6] >> ((tid + 1) & 63) & 1);
-                s_ct = single ? item_positions(batch_own, sh.n_kv, rule.most_positions, p + 1) : prefill_chunk_positions((p / tg + 1) * tg);
+                s_ct = single || rule.tiles ? item_positions(rule, batch_own, (p / tg + 1) * tg) : prefill_chunk_positions((p / tg + 1) * tg);
                 if (!same_seq || p % tg == 0) {
                     s_tok = single ? 1 : min(tg - p % tg, 1 + ones_from(s_goes_on, tid + 1));    // rows of the sequence in its aligned block
                     s_n = (p + s_tok - 1 + s_ct) / s_ct;                                          // chunks the last of them reaches
@@ -191,19 +194,17 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
             cost_items += 7 * ((few ? p_subs : 0) + (single ? s_subs : 0));
             cost_blocks += (few ? 0 : p_subs * 4 + p_subs * 4 / rule.tg_many * p_tok + p_n * 160) + (single ? 0 : s_subs * 4 + s_subs * 4 / rule.tg_many * s_tok + s_n * 160);
         }
-        const int mine[4] = {(few ? p_n : 0) + (single ? s_n : 0), few ? 0 : p_n, single ? 0 : s_n, leads};
-        int start[4];
+        const int mine[3] = {(few ? p_n : 0) + (single ? s_n : 0), few ? 0 : p_n, single ? 0 : s_n};
+        int start[3];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (k < 3 ? FORM != SHARE_LISTS : FORM != SHARE_TILES) continue;
+        for (int k = 0; k < 3; ++k) {
             const int incl = sum_up(mine[k]);
             if (lane == 63) sums[k][wave] = incl;
             start[k] = before[k] + incl - mine[k];
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (k < 3 ? FORM != SHARE_LISTS : FORM != SHARE_TILES) continue;
+        for (int k = 0; k < 3; ++k) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 if (j < wave) start[k] += sums[k][j];
@@ -214,21 +215,19 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
             w.s_seq[t] = r.pos < 0 ? -1 : s_seq;
             w.s_pos[t] = r.pos < 0 ? -1 : p;
             w.p_pos[t] = on ? r.keys - 1 : -1;
-            if constexpr (FORM == SHARE_LISTS) {
-                w.p_seq[t] = on ? r.lead * max_pages : -1;
-                w.p_ct[t] = p_ct;
-                w.s_ct[t] = s_ct;
+            w.p_seq[t] = on ? r.lead * max_pages : -1;
+            w.p_ct[t] = p_ct;
+            w.s_ct[t] = SHARE ? s_ct : rule.most_positions;
+            if constexpr (SHARE) {
                 int32_t *at = few ? w.items + 2 + 2 * (size_t)start[0] : w.p_blocks + 2 + 2 * (size_t)start[1];
                 for (int c = 0; c < p_n; ++c) { *at++ = t; *at++ = c | (p_tok << 20); }
                 at = single ? w.items + 2 + 2 * (size_t)(start[0] + (few ? p_n : 0)) : w.s_blocks + 2 + 2 * (size_t)start[2];
                 for (int c = 0; c < s_n; ++c) { *at++ = single ? t | kOwnItem : t; *at++ = c | (s_tok << 20); }
-            } else {
-                w.p_seq[t] = on ? (r.lead * max_pages) | (few ? kTileNarrow : kTileWide) | (int)((unsigned)(start[3] + leads) << 31) : -1;
             }
         }
         __syncthreads();
     }
-    if constexpr (FORM == SHARE_LISTS) {
+    if constexpr (SHARE) {
         cost_items = sum_all(cost_items);
         cost_blocks = sum_all(cost_blocks);
         if (lane == 0) {
@@ -250,17 +249,17 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
 
 int attn_prefix_max_chunks(int dtype, const AttnShape &sh) {
     const long positions = (long)sh.max_pages_per_seq * sh.page_size;
-    if (!attention_mfma_supported(dtype, sh)) return (sh.max_pages_per_seq + sh.chunk_pages - 1) / sh.chunk_pages;
+    if (!attention_mfma_supported(dtype, sh) && !attn_tile_shape(sh)) return 1;
     const long most = std::max<long>(32, (positions + 8191) / 8192);
     return (int)std::max<long>(1, std::min<long>(most, (positions + 63) / 64));
 }
 
 int attn_own_max_chunks(int dtype, const AttnShape &sh) {
     const int chunks = (sh.max_pages_per_seq + sh.chunk_pages - 1) / sh.chunk_pages;
-    if (!attention_mfma_supported(dtype, sh)) return chunks;
+    if (!attention_mfma_supported(dtype, sh) && !attn_tile_shape(sh)) return chunks;
     const long positions = (long)sh.max_pages_per_seq * sh.page_size;
     const int items = std::max(chunks, (int)std::min<long>(64, (positions + 63) / 64));
-    return std::max(items, attn_prefill_max_chunks(positions));
+    return attention_mfma_supported(dtype, sh) ? std::max(items, attn_prefill_max_chunks(positions)) : items;
 }
 
 size_t attn_shared_plan_words(const AttnShape &sh, const AttnPrefix &prefix, int rows) {
@@ -289,15 +288,10 @@ hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, c
     const int G = sh.n_q / sh.n_kv, TG = G <= 16 ? 16 / G : 1;
     AttnPrefix p = prefix;
     if (p.n_seqs > kShareSeqs) p.lead = nullptr;
-    const dim3 one(1), block(1024);
-    if (form == SHARE_LISTS) {
-        const PlanRule rule{attn_prefill_block_tokens(sh), TG, kFewSharers * TG, sh.chunk_pages * sh.page_size};
-        hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_LISTS>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, rule, w);
-    } else if (form == SHARE_TILES) {
-        hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_TILES>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, PlanRule{4 * TG, TG, TG, 0}, w);
-    } else {
-        hipLaunchKernelGGL(attn_shared_plan_kernel<SHARE_NOTHING>, one, block, 0, s, seq_of_token, pos_of_token, rows, p, sh, PlanRule{1, 1, 0, 0}, w);
-    }
+    const PlanRule rule{form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG, TG, form == SHARE_LISTS ? kFewSharers * TG : TG, sh.chunk_pages * sh.page_size, sh.n_kv,
+                        form == SHARE_TILES};
+    hipLaunchKernelGGL(form == SHARE_NOTHING ? attn_shared_plan_kernel<false> : attn_shared_plan_kernel<true>, dim3(1), dim3(1024), 0, s, seq_of_token, pos_of_token, rows, p,
+                       sh, rule, w);
     return hipGetLastError();
 }
 
