@@ -65,8 +65,14 @@ __device__ __forceinline__ void wait_vm(int n) {   // s_waitcnt vmcnt(n) only
 
 // The items of the multi-token list, claimed until none is left, by a workgroup of kWaves * 64 threads with lds_bytes() of dynamic LDS.
 // PARTS: every item leaves partials for a merge of its own (kernels_attn_shared.hip), also where its chunk is all of what it was given.
-// ld_q: elements from a token's q heads to the next's; 0: rows of the fused projection, k and v heads behind them.
-template <bool PARTS = false>
+// ld_q: elements from a token's q heads to the next's; 0: rows of the fused projection, k and v heads behind them.  Pages may hold a multiple of 16 positions:
+// what is called a page below is a sub-tile of 16 of them, page.per of them to a page.
+struct SubTiles {
+    int per;                           // sub-tiles per page
+    unsigned magic;                    // ceil(2^32 / per)
+    __device__ __forceinline__ int page_of(int sub) const { return (int)__umulhi((unsigned)sub, magic); }     // exact for sub * per below 2^32
+};
+template <bool PARTS = false, bool WIDE_PAGES = false>
 __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qkv,
                                                               const int32_t *__restrict__ seq_of_token,
                                                               const int32_t *__restrict__ pos_of_token,
@@ -76,7 +82,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                                                               bf16_t *__restrict__ out, int ld_out,
                                                               float *__restrict__ part_o, float *__restrict__ part_ml,
                                                               AttnShape sh, const int32_t *__restrict__ plan, int32_t *__restrict__ counter,
-                                                              const int32_t *__restrict__ ct_of_token, int ld_q = 0) {
+                                                              const int32_t *__restrict__ ct_of_token, int ld_q = 0, SubTiles page = SubTiles{}) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int32_t *pid = reinterpret_cast<int32_t *>(lds + kRing * kTile);      // physical pages of the chunk
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -113,7 +119,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
         const int n_tile = (n_pg + kTP - 1) / kTP;
         const int32_t *bt = block_table + (size_t)seq_of_token[t0] * sh.max_pages_per_seq;
 
-        if (tid < chunk_pages) pid[tid] = bt[lp0 + min(tid, n_pg - 1)];
+        if (tid < chunk_pages) pid[tid] = bt[WIDE_PAGES ? page.page_of(lp0 + min(tid, n_pg - 1)) : lp0 + min(tid, n_pg - 1)];
 
         // this wave's columns: B operands of the score product and the keys each column attends
         bf16x8 qb[kSets][4];
@@ -142,18 +148,19 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
         const int wpage = wave & (kTP - 1);
         auto issue = [&](int tile) {
             const int tcl = min(tile, n_tile - 1);                        // past the end: a harmless reload
-            const int pg = pid[min(kTP * tcl + wpage, n_pg - 1)];
+            const int in_chunk = min(kTP * tcl + wpage, n_pg - 1), pg = pid[in_chunk];
+            const int per = WIDE_PAGES ? page.per : 1, slot = WIDE_PAGES ? lp0 + in_chunk - page.page_of(lp0 + in_chunk) * per : 0;     // the sub-tile's place in its page
             unsigned char *dst = lds + (tile % kRing) * kTile + late * (kTP * 4096) + wpage * 4096;
-            const size_t page_elems = ((size_t)pg * sh.n_kv + g) * (PS * HD);
+            const size_t page_elems = ((size_t)pg * sh.n_kv + g) * (PS * HD) * per;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bf16_t *src;
                 if (late) {
                     const int r = j * 32 + (lane >> 1), h = lane & 1;     // V row (head-dim index), 16-byte half in LDS
-                    src = v_cache + page_elems + r * PS + ((h ^ ((r >> 2) & 1)) << 3);
+                    src = v_cache + page_elems + r * PS * per + slot * PS + ((h ^ ((r >> 2) & 1)) << 3);
                 } else {
                     const int r = j * 4 + (lane >> 4), cs = lane & 15;    // K row, 16-byte slot in LDS
-                    src = k_cache + page_elems + r * HD + ((cs ^ (r & 7)) << 3);
+                    src = k_cache + page_elems + (slot * PS + r) * HD + ((cs ^ (r & 7)) << 3);
                 }
                 __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
                                                  (__attribute__((address_space(3))) void *)(dst + j * 1024), 16, 0, 0);

@@ -5,7 +5,7 @@
 
 namespace dyn {
 
-// How rows of a shape are attended: by the forms of this operator (bf16, 128-wide heads, pages of 16), by the layer's general one on the matrix
+// How rows of a shape are attended: by the forms of this operator (bf16, 128-wide heads), by the layer's general one on the matrix
 // cores (attn_tile), or by its plain loops, without sharing.
 enum AttnForm { SHARE_LISTS = 0, SHARE_TILES = 1, SHARE_NOTHING = 2 };
 

@@ -8,6 +8,7 @@
 // (kernels_attn_shared_plan.hip), the keys (attn_shared_kernel, or attn_tile of kernels_attn_generic.hip for what it does not
 // take), and the merge of a row's chunks.
 #include <algorithm>
+#include <atomic>
 
 #include "attn_prefill.h"
 #include "attn_shared_plan.h"
@@ -17,7 +18,7 @@ namespace dyn {
 
 namespace {
 
-constexpr int HD = 128, TILE = 2;         // head dim; sub-tiles of 16 positions (pages) to a register buffer
+constexpr int HD = 128, TILE = 2;         // head dim; sub-tiles of 16 positions to a register buffer
 
 struct SharedArgs {
     const bf16_t *q, *k, *v;
@@ -26,6 +27,7 @@ struct SharedArgs {
     AttnShape sh;                         // rows of a table of one wide row; max_chunks: of both halves
     int ld_q, shared_slots;               // partials of own keys lie behind shared_slots chunks of shared ones
     float *part_o, *part_ml;
+    prefill::SubTiles page;
 };
 
 // One wave's work: up to 16 columns (a token and a q head each) against one chunk of one kv head, all of them seeing all of it.
@@ -43,6 +45,7 @@ struct Item {
 // with the D layout of the first product (lane: column l % 16, positions 4 (l / 16) + r) the B layout of the second.  Two register
 // buffers of 32 positions; the last pair of a chunk is followed by the first of the wave's next item, whose indices were
 // fetched while this one was multiplied.
+template <bool WIDE_PAGES>
 __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int n_blocks, int *taken) {
     const int lane = threadIdx.x & 63, lr = lane & 15, lq = lane >> 4;
     const AttnShape &sh = a.sh;
@@ -81,12 +84,13 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
         constexpr int B = decltype(buf)::value;
 #pragma unroll
         for (int i = 0; i < TILE; ++i) {
-            const size_t page = (size_t)m.table[min(m.first + tile * TILE + i, m.last)] * sh.n_kv + m.g;
-            const bf16_t *kp = a.k + (page * 16 + lr) * HD + 8 * lq, *vp = a.v + (page * HD + lr) * 16 + 4 * lq;
+            const int sub = min(m.first + tile * TILE + i, m.last), per = WIDE_PAGES ? a.page.per : 1, at = WIDE_PAGES ? a.page.page_of(sub) : sub, slot = (sub - at * per) * 16, ps = 16 * per;
+            const size_t page = (size_t)m.table[at] * sh.n_kv + m.g;
+            const bf16_t *kp = a.k + (page * ps + slot + lr) * HD + 8 * lq, *vp = a.v + (page * HD + lr) * ps + slot + 4 * lq;
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) kr[B][i][ks] = *reinterpret_cast<const u32x4 *>(kp + ks * 32);
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) vr[B][i][dt] = *reinterpret_cast<const u32x2 *>(vp + dt * 256);
+            for (int dt = 0; dt < 8; ++dt) vr[B][i][dt] = *reinterpret_cast<const u32x2 *>(vp + dt * 16 * ps);
         }
     };
     auto load_q = [&](bf16x8 (&dst)[4], const Item &m) {
@@ -205,6 +209,7 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
 // All keys of a dispatch in one launch, a workgroup of eight waves per CU: the first claim query blocks (of shared keys, then of own
 // ones), the others serve the items of both and then claim query blocks too.  Items wait for memory and query blocks for the matrix
 // cores (attn_mixed_kernel, kernels_attn_mfma.hip).
+template <bool WIDE_PAGES>
 __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(SharedArgs a) {
     const SharedPlan &w = a.plan;
     __shared__ int taken;
@@ -212,66 +217,67 @@ __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(Sh
     __syncthreads();
     const int groups = gridDim.x, n_blocks = w.p_blocks[0] + w.s_blocks[0];
     const int first = n_blocks == 0 ? 0 : w.items[0] == 0 ? groups : mixed_share(n_blocks * a.sh.n_kv, w.cost[1], w.cost[0], groups);
-    if ((int)blockIdx.x >= first) serve_items(a, (int)blockIdx.x - first, groups - first, &taken);
+    if ((int)blockIdx.x >= first) serve_items<WIDE_PAGES>(a, (int)blockIdx.x - first, groups - first, &taken);
     const size_t behind = part_index(a.sh, 0, 0, a.shared_slots);
 #pragma clang loop unroll(disable)
     for (int own = 0; own < 2; ++own) {
         int32_t *const list = own ? w.s_blocks : w.p_blocks;
         if (list[0] == 0) continue;
-        prefill::attn_prefill_items<true>(a.q, own ? w.s_seq : w.p_seq, own ? w.s_pos : w.p_pos, a.block_table, a.k, a.v, nullptr, 0,
-                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q);
+        prefill::attn_prefill_items<true, WIDE_PAGES>(a.q, own ? w.s_seq : w.p_seq, own ? w.s_pos : w.p_pos, a.block_table, a.k, a.v, nullptr, 0,
+                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q, a.page);
     }
 }
 
-// Merge of a row's partials, shared chunks first, in order: a half-wave per (token, q head), four head-dim indices to a lane, two
-// sets of them in the WIDE form (head dims above 128).  A row without keys is zero.  What it costs is two
-// dependent loads, of the row's chunk counts and of its partials, so the first kMergeLoads of those are on their way beside the maxima and sums
-// that weigh them.
-constexpr int kMergeLoads = 16;
-template <typename T, bool BASE2, bool WIDE>
+// Merge of a row's partials, shared chunks first, in order; four head-dim indices to a lane, two sets of them in the WIDE form (head dims above
+// 128).  Where there are rows to fill the chip a half-wave merges a (token, q head); else (SPLIT) a workgroup does, its eight half-waves every
+// eighth chunk each and the eight results in order through LDS.  A row without keys is zero.  What it costs is two dependent loads, of the row's chunk counts and
+// of its partials, so the first of those are all on their way beside the maxima and sums that weigh them.
+template <typename T, bool BASE2, bool WIDE, bool SPLIT>
 __global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
                                                                   const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
                                                                   const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct,
                                                                   int shared_slots, T *__restrict__ out, int ld_out, AttnShape sh,
                                                                   int32_t *__restrict__ counter0, int32_t *__restrict__ counter1) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    constexpr int SETS = WIDE ? 2 : 1, LOADS = kMergeLoads / SETS;
+    constexpr int SETS = WIDE ? 2 : 1, LOADS = 16 / SETS / (SPLIT ? 2 : 1), STEP = SPLIT ? 8 : 1;
     // the lists' query blocks have all been claimed: from the start again for the next layer
     if (counter0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) *(threadIdx.x ? counter1 : counter0) = 0;
-    const int t = blockIdx.x, sub = threadIdx.x & 31, h = blockIdx.y * 8 + (threadIdx.x >> 5), d = sh.head_dim;
+    const int t = blockIdx.x, sub = threadIdx.x & 31, half = threadIdx.x >> 5, d = sh.head_dim, h = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * 8 + half;
     if (h >= sh.n_q) return;
     const int pp = p_pos[t], sp = s_pos[t], pc = p_ct[t], sc = s_ct[t];
-    const int n_shared = pp < 0 ? 0 : (pp + pc) / pc, n_own = sp < 0 ? 0 : (sp + sc) / sc, n = n_shared + n_own;
-    T *const y = out + (size_t)t * ld_out + h * d;
+    const int n_shared = pp < 0 ? 0 : (pp + pc) / pc, n = n_shared + (sp < 0 ? 0 : (sp + sc) / sc);
+    const int c0 = SPLIT ? half : 0, count = (n - c0 + STEP - 1) / STEP;                     // chunks c0, c0 + STEP, ...
     f32x4 acc[SETS];
 #pragma unroll
     for (int k = 0; k < SETS; ++k) acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float inv = 0.f;
-    if (n) {
+    float M = -INFINITY, L = 0.f;
+    auto weight = [](float x) { return BASE2 ? exp2f(x) : expf(x); };
+    if (count > 0) {
         const size_t first = part_index(sh, t, h, 0), next = sh.n_q;                         // from a chunk to the one behind it
-        auto at = [&](int c) { return first + (size_t)(c < n_shared ? c : shared_slots + c - n_shared) * next; };
-        auto ml_of = [&](int c) { return c < n ? *reinterpret_cast<const f32x2 *>(part_ml + at(c) * 2) : f32x2{-INFINITY, 0.f}; };
+        auto at = [&](int i) {
+            const int c = c0 + i * STEP;
+            return first + (size_t)(c < n_shared ? c : shared_slots + c - n_shared) * next;
+        };
+        auto ml_of = [&](int i) { return i < count ? *reinterpret_cast<const f32x2 *>(part_ml + at(i) * 2) : f32x2{-INFINITY, 0.f}; };
         f32x4 v[LOADS][SETS];
-        auto load = [&](int c0) {
+        auto load = [&](int i0) {
 #pragma unroll
             for (int j = 0; j < LOADS; ++j)
 #pragma unroll
-                for (int k = 0; k < SETS; ++k)
-                    v[j][k] = *reinterpret_cast<const f32x4 *>(part_o + at(min(c0 + j, n - 1)) * d + min(sub * 4 + k * 128, d - 4));
+                for (int k = 0; k < SETS; ++k) v[j][k] = *reinterpret_cast<const f32x4 *>(part_o + at(min(i0 + j, count - 1)) * d + min(sub * 4 + k * 128, d - 4));
         };
         f32x2 ml = ml_of(sub);
         load(0);
-        float M = ml[0];
-        for (int c = sub + 32; c < n; c += 32) M = fmaxf(M, ml_of(c)[0]);
+        M = ml[0];
+        for (int i = sub + 32; i < count; i += 32) M = fmaxf(M, ml_of(i)[0]);
 #pragma unroll
         for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 32));
-        float L = 0.f;
-        for (int cb = 0; cb < n; cb += 32) {
-            if (cb) ml = ml_of(cb + sub);
-            const float dm = ml[0] - M, wgt = BASE2 ? exp2f(dm) : expf(dm);                  // 0 past the last chunk
+        for (int i0 = 0; i0 < count; i0 += 32) {
+            if (i0) ml = ml_of(i0 + sub);
+            const float wgt = weight(ml[0] - M);                                              // 0 past the last chunk
             L += wgt * ml[1];
-            for (int j0 = 0; j0 < 32 && cb + j0 < n; j0 += LOADS) {
-                if (cb + j0) load(cb + j0);
+            for (int j0 = 0; j0 < 32 && i0 + j0 < count; j0 += LOADS) {
+                if (i0 + j0) load(i0 + j0);
 #pragma unroll
                 for (int j = 0; j < LOADS; ++j) {
                     const float wj = __shfl(wgt, j0 + j, 32);
@@ -282,8 +288,33 @@ __global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *_
         }
 #pragma unroll
         for (int off = 16; off >= 1; off >>= 1) L += __shfl_xor(L, off, 32);
-        inv = 1.0f / L;
     }
+    if constexpr (SPLIT) {
+        __shared__ f32x4 split_o[8][32 * SETS];
+        __shared__ float split_ml[8][2];
+#pragma unroll
+        for (int k = 0; k < SETS; ++k) split_o[half][sub + 32 * k] = acc[k];
+        if (sub == 0) { split_ml[half][0] = M; split_ml[half][1] = L; }
+        __syncthreads();
+        if (half) return;
+#pragma unroll
+        for (int j = 1; j < 8; ++j) M = fmaxf(M, split_ml[j][0]);
+        if (n) {
+            const float w0 = weight(split_ml[0][0] - M);
+            L *= w0;
+#pragma unroll
+            for (int k = 0; k < SETS; ++k) acc[k] *= w0;
+#pragma unroll
+            for (int j = 1; j < 8; ++j) {
+                const float w = weight(split_ml[j][0] - M);                                   // 0 of a half-wave without a chunk
+                L += w * split_ml[j][1];
+#pragma unroll
+                for (int k = 0; k < SETS; ++k) acc[k] += split_o[j][sub + 32 * k] * w;
+            }
+        }
+    }
+    const float inv = n ? 1.0f / L : 0.f;
+    T *const y = out + (size_t)t * ld_out + h * d;
 #pragma unroll
     for (int k = 0; k < SETS; ++k) {
         const int i = sub * 4 + k * 128;
@@ -316,17 +347,18 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
     part.max_pages_per_seq = 1;                     // the halves' arrays hold offsets into the table
     part.max_chunks = sh.max_chunks + prefix.max_chunks;
     if (form == SHARE_LISTS) {
-        static bool attr_set = false;
-        if (!attr_set) {
-            e = hipFuncSetAttribute((const void *)attn_shared_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, prefill::lds_bytes());
+        const auto kernel = sh.page_size == 16 ? attn_shared_kernel<false> : attn_shared_kernel<true>;
+        static std::atomic<bool> attr_set[2];
+        if (!attr_set[sh.page_size != 16]) {
+            e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, prefill::lds_bytes());
             if (e != hipSuccess) return e;
-            attr_set = true;
+            attr_set[sh.page_size != 16] = true;
         }
         const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, ld_q, prefix.max_chunks, part_o,
-                           part_ml};
+                           part_ml, prefill::SubTiles{sh.page_size / 16, (unsigned)((0x100000000ull + sh.page_size / 16 - 1) / (sh.page_size / 16))}};
         const long most = (long)rows * sh.n_kv * part.max_chunks;
         const int cus = sh.n_cus > 0 && sh.n_cus < 256 ? sh.n_cus : 256;
-        hipLaunchKernelGGL(attn_shared_kernel, dim3((unsigned)std::min<long>(most, cus)), dim3(prefill::kWaves * 64), prefill::lds_bytes(), s, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<long>(most, cus)), dim3(prefill::kWaves * 64), prefill::lds_bytes(), s, a);
         e = hipGetLastError();
     } else if (form == SHARE_TILES) {
         e = launch_attention_parts(dtype, q, ld_q, block_table, k_cache, v_cache, part_o, part_ml, part, w, prefix.max_chunks, rows, s);
@@ -337,15 +369,19 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
     if (e == hipSuccess && mid) e = hipEventRecord(mid, s);
     if (e != hipSuccess) return e;
     const bool lists = form == SHARE_LISTS;
-    const dim3 grid(rows, (sh.n_q + 7) / 8), block(256);
-#define DYN_COMBINE_AS(T, B2, WIDE)                                                                                                                         \
-    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,                       \
-                       prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, \
-                       lists ? w.s_blocks + 1 : nullptr)
-#define DYN_COMBINE(T, B2)                                      \
-    do {                                                        \
-        if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true);     \
-        else DYN_COMBINE_AS(T, B2, false);                      \
+    // which of the two depends on the batch, so that a row's bits do not depend on the dispatch it is in
+    const bool split = (long)prefix.rows * sh.n_q <= 512;
+    const dim3 grid(rows, split ? sh.n_q : (sh.n_q + 7) / 8), block(256);
+#define DYN_COMBINE_AS(T, B2, WIDE, SPLIT)                                                                                                                  \
+    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE, SPLIT>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,              \
+                       prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, lists ? w.s_blocks + 1 : nullptr)
+#define DYN_COMBINE(T, B2)                                                                                      \
+    do {                                                                                                        \
+        if (split) {                                                                                            \
+            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, true); else DYN_COMBINE_AS(T, B2, false, true);   \
+        } else {                                                                                                \
+            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, false); else DYN_COMBINE_AS(T, B2, false, false); \
+        }                                                                                                       \
     } while (0)
     if (dtype == 0) DYN_COMBINE(float, false);
     else if (form != SHARE_NOTHING) DYN_COMBINE(bf16_t, true);

@@ -18,9 +18,6 @@ int attn_prefill_block_tokens(const AttnShape &sh);
 namespace {
 
 constexpr int kShareSeqs = 4096;              // sequences whose leads are counted in LDS; a batch of more attends without sharing
-// Up to kFewSharers sets of 16 columns (a token and a q head each) of a prefix are served like decodes, K and V read once per set; more by query
-// blocks, which read them once for all.
-constexpr int kFewSharers = 2;
 
 // Inclusive scans over the 64 lanes of a wave on the vector ALU (a shuffle goes through LDS).
 template <int CTRL, int ROWS>
@@ -38,7 +35,7 @@ __device__ __forceinline__ int sum_up(int x) { return scan_wave(x, 0, [](int a, 
 __device__ __forceinline__ int sum_all(int x) { return __builtin_amdgcn_readlane(sum_up(x), 63); }
 
 struct PlanRule {
-    int tg_many, tg_few, most_few;      // tokens of a query block and of an item; the most tokens of a prefix that items serve
+    int tg_many, tg_few;                // tokens of a query block and of an item
     int most_positions;                 // the longest chunk of a single token's own keys
     int n_kv;
     bool tiles;                         // SHARE_TILES
@@ -57,6 +54,15 @@ __device__ __forceinline__ int block_positions(const PlanRule &rule, long long s
 __device__ __forceinline__ int item_positions(const PlanRule &rule, long long own, int keys) {
     const long long want = own * rule.n_kv / (rule.tiles ? 128 : 512), least = rule.tiles ? 128 : 64;
     return (int)max(min(max((want + 63) / 64 * 64, least), (long long)rule.most_positions), ((long long)keys / 64 + 63) / 64 * 64);
+}
+
+// Whether a prefix that `tokens` tokens attend is served by items, which read K and V once for every tg_few of them, and not by query blocks, which read
+// them once for all.  In time of a CU, a position of an item takes some 17 ns, of a query block 15 ns, and 10 us around a block and chunk, in which all of
+// the CU waits for its claim, its pages, its first tile and its stores: items where they are no more than that, and all by items where the batch's
+// would take the chip no longer than a block's 14 us.  `batch` = sub-tiles of shared keys over tokens.  General form: by items up to one set of columns.
+__device__ __forceinline__ bool by_items(const PlanRule &rule, long long batch, int tokens, int chunk) {
+    const long long sets = (tokens + rule.tg_few - 1) / rule.tg_few;
+    return rule.tiles ? sets <= 1 : batch * rule.n_kv < 13000 * rule.tg_few || 17 * sets * chunk < 10000 + 15 * chunk;
 }
 
 // Set bits from bit `at` on, as far as they follow one another.
@@ -168,13 +174,16 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
             run_before = max(run_before, sums[4][k]);
         }
         if (tid == 0) { edge_lead[0] = edge_lead[16]; edge_keys[0] = edge_keys[16]; edge_seq[0] = edge_seq[16]; }   // (read again behind the next barriers)
-        const bool few = on && members[r.lead] <= rule.most_few;
+        int p_tok = 0, p_n = 0, p_ct = 64, s_tok = 0, s_n = 0, s_ct = 64;              // what row t leads: tokens and chunks
+        bool few = false, single = false;
+        if (on) {
+            p_ct = block_positions(rule, batch_shared, batch_own, r.keys);
+            few = by_items(rule, batch[0], members[r.lead], p_ct);
+            if (few) p_ct = item_positions(rule, batch_own, 2 * r.keys);
+        }
         const int width = few ? rule.tg_few : rule.tg_many;
         const bool leads = on && (t - run) % width == 0;
-        int p_tok = 0, p_n = 0, p_ct = 64, s_tok = 0, s_n = 0, s_ct = 64;              // what row t leads: tokens and chunks
-        bool single = false;
         if constexpr (SHARE) {
-            if (on) p_ct = few ? item_positions(rule, batch_own, 2 * r.keys) : block_positions(rule, batch_shared, batch_own, r.keys);
             if (leads) {
                 p_tok = min(width, 1 + ones_from(p_goes_on, tid + 1));
                 p_n = (r.keys - 1 + p_ct) / p_ct;
@@ -247,19 +256,26 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
 
 }  // namespace
 
+// The shapes that the forms of this operator take: the layer's fast ones, and larger pages.
+static bool lists_shape(int dtype, const AttnShape &sh) {
+    AttnShape small = sh;
+    if (sh.page_size % 16 == 0) small.page_size = 16;
+    return attention_mfma_supported(dtype, small);
+}
+
 int attn_prefix_max_chunks(int dtype, const AttnShape &sh) {
     const long positions = (long)sh.max_pages_per_seq * sh.page_size;
-    if (!attention_mfma_supported(dtype, sh) && !attn_tile_shape(sh)) return 1;
+    if (!lists_shape(dtype, sh) && !attn_tile_shape(sh)) return 1;
     const long most = std::max<long>(32, (positions + 8191) / 8192);
     return (int)std::max<long>(1, std::min<long>(most, (positions + 63) / 64));
 }
 
 int attn_own_max_chunks(int dtype, const AttnShape &sh) {
     const int chunks = (sh.max_pages_per_seq + sh.chunk_pages - 1) / sh.chunk_pages;
-    if (!attention_mfma_supported(dtype, sh) && !attn_tile_shape(sh)) return chunks;
+    if (!lists_shape(dtype, sh) && !attn_tile_shape(sh)) return chunks;
     const long positions = (long)sh.max_pages_per_seq * sh.page_size;
     const int items = std::max(chunks, (int)std::min<long>(64, (positions + 63) / 64));
-    return attention_mfma_supported(dtype, sh) ? std::max(items, attn_prefill_max_chunks(positions)) : items;
+    return lists_shape(dtype, sh) ? std::max(items, attn_prefill_max_chunks(positions)) : items;
 }
 
 size_t attn_shared_plan_words(const AttnShape &sh, const AttnPrefix &prefix, int rows) {
@@ -280,7 +296,7 @@ SharedPlan attn_shared_plan(int32_t *plan, const AttnShape &sh, const AttnPrefix
 }
 
 AttnForm attn_shared_form(int dtype, const AttnShape &sh, const void *k_cache, const void *v_cache) {
-    return attention_mfma_supported(dtype, sh) ? SHARE_LISTS : attn_tile_takes(sh, k_cache, v_cache) ? SHARE_TILES : SHARE_NOTHING;
+    return lists_shape(dtype, sh) && !(((uintptr_t)k_cache | (uintptr_t)v_cache) & 15) ? SHARE_LISTS : attn_tile_takes(sh, k_cache, v_cache) ? SHARE_TILES : SHARE_NOTHING;
 }
 
 hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, const int32_t *pos_of_token, const AttnShape &sh, const AttnPrefix &prefix, int rows,
@@ -288,7 +304,7 @@ hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, c
     const int G = sh.n_q / sh.n_kv, TG = G <= 16 ? 16 / G : 1;
     AttnPrefix p = prefix;
     if (p.n_seqs > kShareSeqs) p.lead = nullptr;
-    const PlanRule rule{form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG, TG, form == SHARE_LISTS ? kFewSharers * TG : TG, sh.chunk_pages * sh.page_size, sh.n_kv,
+    const PlanRule rule{form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG, TG, sh.chunk_pages * sh.page_size, sh.n_kv,
                         form == SHARE_TILES};
     hipLaunchKernelGGL(form == SHARE_NOTHING ? attn_shared_plan_kernel<false> : attn_shared_plan_kernel<true>, dim3(1), dim3(1024), 0, s, seq_of_token, pos_of_token, rows, p,
                        sh, rule, w);

@@ -19,6 +19,7 @@ DEV = "cuda:0"
 SHAPES = {
     "fast": (8, 2, 128, 16, torch.bfloat16), "fast_g3": (6, 2, 128, 16, torch.bfloat16), "fast_g1": (3, 3, 128, 16, torch.bfloat16),
     "fast_g16": (16, 1, 128, 16, torch.bfloat16),
+    "fast_p48": (8, 2, 128, 48, torch.bfloat16), "fast_p512": (4, 2, 128, 512, torch.bfloat16),
     "bf16_64": (8, 2, 64, 16, torch.bfloat16), "bf16_p32": (8, 2, 128, 32, torch.bfloat16), "bf16_256": (4, 2, 256, 16, torch.bfloat16),
     "f32_64": (8, 2, 64, 16, torch.float32), "f32_32": (3, 1, 32, 48, torch.float32), "f32_128": (4, 4, 128, 16, torch.float32),
     "odd_page": (4, 2, 64, 5, torch.float32), "narrow": (4, 2, 8, 16, torch.bfloat16), "many_heads": (34, 2, 32, 16, torch.bfloat16),
@@ -149,7 +150,7 @@ def test_groups_of_every_size_beside_sequences_alone(shape):
     say("%s: worst share of the bound %.2f" % (shape, c.check(c.run())))
 
 
-@pytest.mark.parametrize("shape", ["fast", "fast_g3", "bf16_64", "f32_64", "odd_page"])
+@pytest.mark.parametrize("shape", ["fast", "fast_g3", "fast_p48", "bf16_p32", "bf16_64", "f32_64", "odd_page"])
 def test_several_tokens_a_sequence(shape):
     """Drafts of a few tokens, prompts of many, behind a shared prefix, beside decodes of the same group."""
     seqs = (group("a", 9, [5, 1, 90, 200, 3, 64]) + group("a", 9, [30, 150, 4], new=3) + [("a", 9, 170, 150), ("a", 9, 40, 40)] + group("b", 3, [25] * 12, new=5) +
@@ -158,7 +159,7 @@ def test_several_tokens_a_sequence(shape):
     c.check(c.run())
 
 
-@pytest.mark.parametrize("shape,shared", [("fast", 300), ("fast", 531), ("bf16_64", 150), ("f32_64", 70)])
+@pytest.mark.parametrize("shape,shared", [("fast", 300), ("fast", 531), ("fast_p48", 111), ("bf16_64", 150), ("f32_64", 70)])
 @pytest.mark.parametrize("n", [2, 7, 9, 40])
 def test_long_prefixes(shape, shared, n):
     """Prefixes of many chunks, odd page counts, few and many sharers."""
