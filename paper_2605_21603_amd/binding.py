@@ -563,7 +563,8 @@ class DeviceStep:
 
 
 def _stream_of(stream: Optional[torch.cuda.Stream], device) -> C.c_void_p:
-    return C.c_void_p((stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream)
+    # (the raw handle: building torch's Stream object takes 2 us, as long as a small call's kernel)
+    return C.c_void_p(stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index))
 
 
 def _int32(t: torch.Tensor, name: str, device, shape) -> int:

@@ -15,13 +15,24 @@ namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 constexpr int kScan = 16;                       // pages a thread looks at per round of a search
+constexpr int kNearRows = 8192, kNearFresh = 2048;   // rows whose requests are told apart in LDS, and pages found that are kept there
 
-template <typename T>
-__device__ __forceinline__ T wave_scan(T x) {
+// Inclusive sums over the 64 lanes of a wave: on the vector ALU in 32 bits (a shuffle goes through LDS), else by shuffles.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int x) {
+    x += moved<0x111, 0xf>(x);                  // row_shr 1, 2, 4, 8
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);                  // row_bcast 15: rows 1 and 3 take the row below's last
+    return x + moved<0x143, 0xc>(x);            // row_bcast 31: rows 2 and 3 take lane 31's
+}
+__device__ __forceinline__ long long wave_scan(long long x) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const T y = __shfl_up(x, off, 64);
+        const long long y = __shfl_up(x, off, 64);
         if (lane >= off) x += y;
     }
     return x;
@@ -47,28 +58,30 @@ __device__ __forceinline__ T before_me(T x, T *lds, T *total) {
 
 // The pages of begin .. end - 1 whose count `wanted` accepts, in ascending order: take(rank, page) for each of rank below `limit`.
 // Returns how many there are, or any number from `limit` on.  What a round takes is its loads' latency, so the next round's are on their way while
-// one is ranked.  lds: kScan * kPlanWaves + 1 words.
-template <class Wanted, class Take>
-__device__ __forceinline__ int ranked_pages(const int32_t *ref, int begin, int end, int limit, int *lds, Wanted &&wanted, Take &&take) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int found = 0, count[kScan];
-    auto load = [&](int at) {
+// one is ranked; count: the first round's (load_round).  lds: kScan * kPlanWaves + 1 words.
+struct Round { int count[kScan]; };
+__device__ __forceinline__ Round load_round(const int32_t *ref, int at, int end) {
+    Round r;
 #pragma unroll
-        for (int j = 0; j < kScan; ++j) {
-            const int p = at + j * kPlanThreads + (int)threadIdx.x;
-            count[j] = p < end ? ref[p] : 0;
-        }
-    };
-    if (begin < end) load(begin);
+    for (int j = 0; j < kScan; ++j) {
+        const int p = at + j * kPlanThreads + (int)threadIdx.x;
+        r.count[j] = p < end ? ref[p] : 0;
+    }
+    return r;
+}
+template <class Wanted, class Take>
+__device__ __forceinline__ int ranked_pages(const int32_t *ref, int begin, int end, int limit, int *lds, Round round, Wanted &&wanted, Take &&take) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int found = 0;
     for (int at = begin; at < end && found < limit; at += kScan * kPlanThreads) {
         unsigned long long mask[kScan];
 #pragma unroll
         for (int j = 0; j < kScan; ++j) {
             const int p = at + j * kPlanThreads + (int)threadIdx.x;
-            mask[j] = __ballot(p < end && wanted(count[j], p));
+            mask[j] = __ballot(p < end && wanted(round.count[j], p));
             if (lane == 0) lds[j * kPlanWaves + wave] = __popcll(mask[j]);
         }
-        if (end - at > kScan * kPlanThreads) load(at + kScan * kPlanThreads);
+        if (end - at > kScan * kPlanThreads) round = load_round(ref, at + kScan * kPlanThreads, end);
         __syncthreads();
         if (wave == 0) {                        // exclusive sums of the round's kScan x kPlanWaves counts, four to a lane
             int v[4], sum = 0;
@@ -97,16 +110,16 @@ static_assert(kScan * kPlanWaves == 4 * 64, "a wave sums a round's counts, four 
 struct Request { int status, had, has, need, copy, length; };
 
 template <bool FORK>
-__device__ __forceinline__ Request look_at(const PageTables &t, const int32_t *owner, int i, int x, int y) {
+__device__ __forceinline__ Request look_at(const PageTables &t, bool mine, int x, int y) {
     Request r{PAGES_REFUSED, 0, 0, 0, -1, 0};
     bool part = false;                          // the request copies a page
     const int ps = t.page_size, row = FORK ? y : x;
     const long long most = (long long)t.max_pages * ps;
-    if (row < 0 || row >= t.n_rows || __hip_atomic_load(&owner[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i) return r;
-    const int mine = t.seq_len[row];
-    if (mine < 0 || mine > most) return r;
+    if (!mine) return r;
+    const int had = t.seq_len[row];
+    if (had < 0 || had > most) return r;
     if constexpr (FORK) {
-        if (x < 0 || x >= t.n_rows || x == y || mine != 0) return r;
+        if (x < 0 || x >= t.n_rows || x == y || had != 0) return r;
         const int len = t.seq_len[x];
         if (len < 0 || len > most) return r;
         r.had = len / ps;
@@ -116,11 +129,11 @@ __device__ __forceinline__ Request look_at(const PageTables &t, const int32_t *o
         if (part) r.copy = t.block_table[(size_t)x * t.max_pages + r.had];
     } else {
         if (y < 0 || y > most) return r;
-        r.had = (int)(((long long)mine + ps - 1) / ps);
+        r.had = (int)(((long long)had + ps - 1) / ps);
         r.has = (int)(((long long)y + ps - 1) / ps);
         r.length = y;
         r.need = max(r.has - r.had, 0);
-        if (y < mine && y % ps) {               // a partly filled page stays: it must be the row's own
+        if (y < had && y % ps) {               // a partly filled page stays: it must be the row's own
             const int last = t.block_table[(size_t)x * t.max_pages + r.has - 1];
             if (last < 0 || last >= t.n_pages) return r;
             part = t.ref_count[last] > 1;
@@ -141,57 +154,84 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PageTables t, 
                                                                   const int32_t *__restrict__ ys, int32_t *__restrict__ status) {
     __shared__ int lds[kScan * kPlanWaves + 1];
     __shared__ long long lds_need[kPlanWaves];
+    __shared__ int owner_near[kNearRows], fresh_near[kNearFresh];
+    const Round first_round = load_round(t.ref_count, 0, t.n_pages);     // on its way beside the requests
     // a row that several requests name is the first one's
     const int32_t *rows = FORK ? ys : xs;
-    for (int i = threadIdx.x; i < n; i += kPlanThreads)
-        if (rows[i] >= 0 && rows[i] < t.n_rows) w.owner[rows[i]] = n;
-    __threadfence_block();
+    const bool near = t.n_rows <= kNearRows;
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+        const int row = rows[i];
+        if (row >= 0 && row < t.n_rows) (near ? owner_near : w.owner)[row] = n;
+    }
+    if (!near) __threadfence_block();
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads)
-        if (rows[i] >= 0 && rows[i] < t.n_rows) atomicMin(&w.owner[rows[i]], i);
-    __threadfence_block();
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+        const int row = rows[i];
+        if (row < 0 || row >= t.n_rows) continue;
+        if (near) atomicMin(&owner_near[row], i);
+        else atomicMin(&w.owner[row], i);
+    }
+    if (!near) __threadfence_block();
     __syncthreads();
-    long long wanted = 0;                       // pages all requests so far take together
+    const bool narrow = t.max_pages <= 1 << 20;  // what a batch of requests asks for fits 32 bits
+    long long wanted = 0;                        // pages all requests so far take together
+    Request kept{PAGES_REFUSED, 0, 0, 0, -1, 0}; // the first batch's, and where its pages start, stay in registers
+    int kept_first = -2;
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + (int)threadIdx.x;
         Request r{PAGES_REFUSED, 0, 0, 0, -1, 0};
-        if (i < n) r = look_at<FORK>(t, w.owner, i, xs[i], ys[i]);
-        const int need = r.status == PAGES_DONE ? r.need : 0;
-        long long total;
-        const long long first = wanted + before_me((long long)need, lds_need, &total);
         if (i < n) {
-            w.first[i] = r.status != PAGES_DONE ? -2 : !need ? 0 : first + need > t.n_pages ? -1 : (int)first;
+            const int row = rows[i];
+            bool mine = row >= 0 && row < t.n_rows;
+            if (mine) mine = (near ? owner_near[row] : __hip_atomic_load(&w.owner[row], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == i;
+            r = look_at<FORK>(t, mine, xs[i], ys[i]);
+        }
+        const int need = r.status == PAGES_DONE ? r.need : 0;
+        long long first = wanted;
+        if (narrow) {
+            int total;
+            first += before_me(need, lds, &total);
+            wanted += total;
+        } else {
+            long long total;
+            first += before_me((long long)need, lds_need, &total);
+            wanted += total;
+        }
+        const int at = r.status != PAGES_DONE ? -2 : !need ? 0 : first + need > t.n_pages ? -1 : (int)first;
+        if (i0 == 0) { kept = r; kept_first = at; }
+        if (i < n) {
             w.had[i] = r.had;
             w.has[i] = r.has;
-            w.need[i] = need;
             w.length[i] = r.length;
             w.src[i] = r.copy;
+            if (i0) { w.first[i] = at; w.need[i] = need; }
         }
-        wanted += total;
     }
-    __threadfence_block();
-    __syncthreads();
     const int limit = (int)min(wanted, (long long)t.n_pages);
-    const int found = limit ? ranked_pages(t.ref_count, 0, t.n_pages, limit, lds, [](int count, int) { return count == 0; },
-                                           [&](int rank, int p) { w.fresh[rank] = p; }) : 0;
-    __threadfence_block();
+    const int found = limit ? ranked_pages(t.ref_count, 0, t.n_pages, limit, lds, first_round, [](int count, int) { return count == 0; },
+                                           [&](int rank, int p) {
+                                               w.fresh[rank] = p;
+                                               if (rank < kNearFresh) fresh_near[rank] = p;
+                                           }) : 0;
+    if (limit > kNearFresh || n > kPlanThreads) __threadfence_block();      // only then is read below what others wrote to memory
     __syncthreads();
     int copies = 0;
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + (int)threadIdx.x;
         int src = -1, first = -2;
         if (i < n) {
-            first = w.first[i];
-            if (first >= 0 && w.need[i] && first + w.need[i] > found) first = -1;
+            first = i0 ? w.first[i] : kept_first;
+            const int need = i0 ? w.need[i] : kept.need;
+            if (first >= 0 && need && first + need > found) first = -1;
             w.first[i] = first;
             status[i] = first >= 0 ? PAGES_DONE : first == -1 ? PAGES_NONE_LEFT : PAGES_REFUSED;
-            if (first >= 0) src = w.src[i];
+            if (first >= 0) src = i0 ? w.src[i] : kept.copy;
         }
         int total;
         const int at = copies + before_me(src >= 0 ? 1 : 0, lds, &total);
         if (src >= 0) {
             w.copy_src[at] = src;
-            w.copy_dst[at] = w.fresh[first];
+            w.copy_dst[at] = first < kNearFresh ? fresh_near[first] : w.fresh[first];
         }
         copies += total;
     }
@@ -203,12 +243,17 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_plan_kernel(PageTa
                                                                           int32_t *__restrict__ n_live) {
     __shared__ int lds[kScan * kPlanWaves + 1];
     const int n = t.n_pages, all = n + 1;
-    const int live = ranked_pages(t.ref_count, 0, n, all, lds, [&](int count, int p) {
+    const Round first = load_round(t.ref_count, 0, n);
+    const int live = ranked_pages(t.ref_count, 0, n, all, lds, first, [&](int count, int p) {
         new_page[p] = count > 0 ? p : -1;
         return count > 0;
     }, [](int, int) {});
-    ranked_pages(t.ref_count, 0, live, all, lds, [](int count, int) { return count <= 0; }, [&](int rank, int p) { w.copy_dst[rank] = p; });
-    const int moves = ranked_pages(t.ref_count, live, n, all, lds, [](int count, int) { return count > 0; }, [&](int rank, int p) { w.copy_src[rank] = p; });
+    const bool once = n <= kScan * kPlanThreads;                 // the counts are all in registers
+    const Round behind = once ? first : load_round(t.ref_count, live, n);
+    ranked_pages(t.ref_count, 0, live, all, lds, once ? first : load_round(t.ref_count, 0, live), [](int count, int) { return count <= 0; },
+                 [&](int rank, int p) { w.copy_dst[rank] = p; });
+    const int moves = ranked_pages(t.ref_count, once ? 0 : live, n, all, lds, behind, [&](int count, int p) { return p >= live && count > 0; },
+                                   [&](int rank, int p) { w.copy_src[rank] = p; });
     __threadfence_block();
     __syncthreads();
     for (int i = threadIdx.x; i < moves; i += kPlanThreads) {
