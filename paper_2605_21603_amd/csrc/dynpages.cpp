@@ -109,7 +109,7 @@ dyn_status plan_and_apply(const dyn_page_pool *p, int what, const char *name, co
     hipError_t e = dyn::launch_pages_plan(what, t, plan, n, xs, ys, status, new_page, n_live, s);
     if (e == hipSuccess) e = dyn::launch_pages_apply(what, t, plan, layers_from(p, 0), rows, most_copies, xs, ys, new_page, s);
     for (int l0 = dyn::kPageLayers; l0 < p->n_layers && e == hipSuccess; l0 += dyn::kPageLayers)
-        e = dyn::launch_pages_copy(layers_from(p, l0), p->n_pages, (int)most_copies, plan.copy_src, plan.copy_dst, plan.n_copies, s);
+        e = dyn::launch_pages_copy(what == dyn::PAGES_COMPACT, layers_from(p, l0), p->n_pages, (int)most_copies, plan.copy_src, plan.copy_dst, plan.n_copies, s);
     return launched(e, name);
 }
 
@@ -129,7 +129,7 @@ dyn_status dyn_pages_copy(const dyn_page_pool *p, int n, const int32_t *src, con
     if (n == 0) return DYN_OK;
     if (!src || !dst) return fail(DYN_ERR_INVALID_ARG, "NULL argument");
     for (int l0 = 0; l0 < p->n_layers && rc == DYN_OK; l0 += dyn::kPageLayers)
-        rc = launched(dyn::launch_pages_copy(layers_from(p, l0), p->n_pages, n, src, dst, nullptr, (hipStream_t)hip_stream), "page copy");
+        rc = launched(dyn::launch_pages_copy(true, layers_from(p, l0), p->n_pages, n, src, dst, nullptr, (hipStream_t)hip_stream), "page copy");
     return rc;
 }
 

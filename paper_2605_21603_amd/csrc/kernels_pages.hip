@@ -14,7 +14,9 @@ namespace dyn {
 namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-constexpr int kScan = 16;                       // pages a thread looks at per round of a search
+// Pages a thread looks at per round of a search (SCAN): 4, or 16 in pools of more than four such rounds, where a round's latency is what counts.  (Plan and
+// all of a fork into 7, 16 -> 4: 31.0 -> 28.7 us.)
+constexpr int kScanNear = 4, kScanFar = 16;
 constexpr int kNearRows = 8192, kNearFresh = 2048;   // rows whose requests are told apart in LDS, and pages found that are kept there
 
 // Inclusive sums over the 64 lanes of a wave: on the vector ALU in 32 bits (a shuffle goes through LDS), else by shuffles.
@@ -58,52 +60,54 @@ __device__ __forceinline__ T before_me(T x, T *lds, T *total) {
 
 // The pages of begin .. end - 1 whose count `wanted` accepts, in ascending order: take(rank, page) for each of rank below `limit`.
 // Returns how many there are, or any number from `limit` on.  What a round takes is its loads' latency, so the next round's are on their way while
-// one is ranked; count: the first round's (load_round).  lds: kScan * kPlanWaves + 1 words.
-struct Round { int count[kScan]; };
-__device__ __forceinline__ Round load_round(const int32_t *ref, int at, int end) {
-    Round r;
+// one is ranked; round: the first one (load_round).  lds: SCAN * kPlanWaves + 1 words.
+template <int SCAN>
+struct Round { int count[SCAN]; };
+template <int SCAN>
+__device__ __forceinline__ Round<SCAN> load_round(const int32_t *ref, int at, int end) {
+    Round<SCAN> r;
 #pragma unroll
-    for (int j = 0; j < kScan; ++j) {
+    for (int j = 0; j < SCAN; ++j) {
         const int p = at + j * kPlanThreads + (int)threadIdx.x;
         r.count[j] = p < end ? ref[p] : 0;
     }
     return r;
 }
-template <class Wanted, class Take>
-__device__ __forceinline__ int ranked_pages(const int32_t *ref, int begin, int end, int limit, int *lds, Round round, Wanted &&wanted, Take &&take) {
+template <int SCAN, class Wanted, class Take>
+__device__ __forceinline__ int ranked_pages(const int32_t *ref, int begin, int end, int limit, int *lds, Round<SCAN> round, Wanted &&wanted, Take &&take) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int found = 0;
-    for (int at = begin; at < end && found < limit; at += kScan * kPlanThreads) {
-        unsigned long long mask[kScan];
+    for (int at = begin; at < end && found < limit; at += SCAN * kPlanThreads) {
+        unsigned long long mask[SCAN];
 #pragma unroll
-        for (int j = 0; j < kScan; ++j) {
+        for (int j = 0; j < SCAN; ++j) {
             const int p = at + j * kPlanThreads + (int)threadIdx.x;
             mask[j] = __ballot(p < end && wanted(round.count[j], p));
             if (lane == 0) lds[j * kPlanWaves + wave] = __popcll(mask[j]);
         }
-        if (end - at > kScan * kPlanThreads) round = load_round(ref, at + kScan * kPlanThreads, end);
+        if (end - at > SCAN * kPlanThreads) round = load_round<SCAN>(ref, at + SCAN * kPlanThreads, end);
         __syncthreads();
-        if (wave == 0) {                        // exclusive sums of the round's kScan x kPlanWaves counts, four to a lane
-            int v[4], sum = 0;
+        if (wave == 0) {                        // exclusive sums of the round's SCAN x kPlanWaves counts, kPerLane to a lane
+            constexpr int kPerLane = SCAN * kPlanWaves / 64;
+            int v[kPerLane], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = sum; sum += lds[4 * lane + i]; }
+            for (int i = 0; i < kPerLane; ++i) { v[i] = sum; sum += lds[kPerLane * lane + i]; }
             const int incl = wave_scan(sum);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) lds[4 * lane + i] = v[i] + incl - sum;
-            if (lane == 63) lds[kScan * kPlanWaves] = incl;
+            for (int i = 0; i < kPerLane; ++i) lds[kPerLane * lane + i] = v[i] + incl - sum;
+            if (lane == 63) lds[SCAN * kPlanWaves] = incl;
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kScan; ++j) {
+        for (int j = 0; j < SCAN; ++j) {
             const int rank = found + lds[j * kPlanWaves + wave] + __popcll(mask[j] & ((1ull << lane) - 1));
             if ((mask[j] >> lane & 1) && rank < limit) take(rank, at + j * kPlanThreads + (int)threadIdx.x);
         }
-        found += lds[kScan * kPlanWaves];
+        found += lds[SCAN * kPlanWaves];
         __syncthreads();
     }
     return found;
 }
-static_assert(kScan * kPlanWaves == 4 * 64, "a wave sums a round's counts, four to a lane");
 
 // One request as the search sees it.  had, has: pages its row keeps (fork: shares), and has behind the call; need: pages it takes; copy: the page
 // whose content goes into the first of them, -1: none.
@@ -149,13 +153,13 @@ __device__ __forceinline__ Request look_at(const PageTables &t, bool mine, int x
 }
 
 // One workgroup.  Requests in order: who is served, which free pages go to whom, which pages are copied.
-template <bool FORK>
+template <bool FORK, int SCAN>
 __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PageTables t, PagesPlan w, int n, const int32_t *__restrict__ xs,
                                                                   const int32_t *__restrict__ ys, int32_t *__restrict__ status) {
-    __shared__ int lds[kScan * kPlanWaves + 1];
+    __shared__ int lds[SCAN * kPlanWaves + 1];
     __shared__ long long lds_need[kPlanWaves];
     __shared__ int owner_near[kNearRows], fresh_near[kNearFresh];
-    const Round first_round = load_round(t.ref_count, 0, t.n_pages);     // on its way beside the requests
+    const Round<SCAN> first_round = load_round<SCAN>(t.ref_count, 0, t.n_pages);     // on its way beside the requests
     // a row that several requests name is the first one's
     const int32_t *rows = FORK ? ys : xs;
     const bool near = t.n_rows <= kNearRows;
@@ -239,18 +243,19 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PageTables t, 
 }
 
 // One workgroup.  Every live page from the n_live-th on moves to a free one below it, the lowest to the lowest.
+template <int SCAN>
 __global__ __launch_bounds__(kPlanThreads) void pages_compact_plan_kernel(PageTables t, PagesPlan w, int32_t *__restrict__ new_page,
                                                                           int32_t *__restrict__ n_live) {
-    __shared__ int lds[kScan * kPlanWaves + 1];
+    __shared__ int lds[SCAN * kPlanWaves + 1];
     const int n = t.n_pages, all = n + 1;
-    const Round first = load_round(t.ref_count, 0, n);
+    const Round<SCAN> first = load_round<SCAN>(t.ref_count, 0, n);
     const int live = ranked_pages(t.ref_count, 0, n, all, lds, first, [&](int count, int p) {
         new_page[p] = count > 0 ? p : -1;
         return count > 0;
     }, [](int, int) {});
-    const bool once = n <= kScan * kPlanThreads;                 // the counts are all in registers
-    const Round behind = once ? first : load_round(t.ref_count, live, n);
-    ranked_pages(t.ref_count, 0, live, all, lds, once ? first : load_round(t.ref_count, 0, live), [](int count, int) { return count <= 0; },
+    const bool once = n <= SCAN * kPlanThreads;                 // the counts are all in registers
+    const Round<SCAN> behind = once ? first : load_round<SCAN>(t.ref_count, live, n);
+    ranked_pages(t.ref_count, 0, live, all, lds, once ? first : load_round<SCAN>(t.ref_count, 0, live), [](int count, int) { return count <= 0; },
                  [&](int rank, int p) { w.copy_dst[rank] = p; });
     const int moves = ranked_pages(t.ref_count, once ? 0 : live, n, all, lds, behind, [&](int count, int p) { return p >= live && count > 0; },
                                    [&](int rank, int p) { w.copy_src[rank] = p; });
@@ -267,7 +272,10 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_plan_kernel(PageTa
 
 constexpr int kCopyThreads = 256, kCopyVec = 4, kPiece = kCopyThreads * kCopyVec * 16;       // bytes a workgroup copies at a time
 
-// Pieces of the listed pages, in every layer, dealt to the workgroups `block` of `n_blocks`.
+// Pieces of the listed pages, in every layer, dealt to the workgroups `block` of `n_blocks`.  What bounds it is memory, read and written once: 389
+// pages of 32 layers (1.63 GB) at 5.07 TB/s.  Stores go past the caches (they are 2 % slower through them), and so do loads where every page is read once (ONCE:
+// another 2 %); a fork's page goes to several children and is read from a cache for all but one (60 pages of 17 layers to 3 children each: 314 -> 262 us).
+template <bool ONCE>
 __device__ __forceinline__ void copy_pages(const PageLayers &l, int n_pages, const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int copies, int block,
                                            int n_blocks) {
     const unsigned pieces = (unsigned)((l.page_bytes + kPiece - 1) / kPiece), per_copy = 2u * l.n * pieces;
@@ -281,18 +289,23 @@ __device__ __forceinline__ void copy_pages(const PageLayers &l, int n_pages, con
         const char *const s = base + (size_t)from * l.page_bytes;
         char *const d = base + (size_t)to * l.page_bytes;
         u32x4 v[kCopyVec];
+        auto load = [](const char *p) {
+            if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+            else return *reinterpret_cast<const u32x4 *>(p);
+        };
 #pragma unroll
         for (int j = 0; j < kCopyVec; ++j)
-            if (at + j * kCopyThreads * 16 < l.page_bytes) v[j] = *reinterpret_cast<const u32x4 *>(s + at + j * kCopyThreads * 16);
+            if (at + j * kCopyThreads * 16 < l.page_bytes) v[j] = load(s + at + j * kCopyThreads * 16);
 #pragma unroll
         for (int j = 0; j < kCopyVec; ++j)
-            if (at + j * kCopyThreads * 16 < l.page_bytes) *reinterpret_cast<u32x4 *>(d + at + j * kCopyThreads * 16) = v[j];
+            if (at + j * kCopyThreads * 16 < l.page_bytes) __builtin_nontemporal_store(v[j], reinterpret_cast<u32x4 *>(d + at + j * kCopyThreads * 16));
     }
 }
 
+template <bool ONCE>
 __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(PageLayers l, int n_pages, const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
                                                                   const int32_t *__restrict__ n_copies, int n) {
-    copy_pages(l, n_pages, src, dst, n_copies ? *n_copies : n, blockIdx.x, gridDim.x);
+    copy_pages<ONCE>(l, n_pages, src, dst, n_copies ? *n_copies : n, blockIdx.x, gridDim.x);
 }
 
 // The first `tables` workgroups write rows, lengths and counts (a request each), the others copy pages.  tables = 0: pages only.
@@ -300,7 +313,7 @@ template <int WHAT>
 __global__ __launch_bounds__(kCopyThreads) void pages_apply_kernel(PageTables t, PagesPlan w, PageLayers l, int n, int tables, const int32_t *__restrict__ xs,
                                                                    const int32_t *__restrict__ ys, const int32_t *__restrict__ new_page) {
     if ((int)blockIdx.x >= tables) {
-        copy_pages(l, t.n_pages, w.copy_src, w.copy_dst, *w.n_copies, (int)blockIdx.x - tables, (int)gridDim.x - tables);
+        copy_pages<WHAT == PAGES_COMPACT>(l, t.n_pages, w.copy_src, w.copy_dst, *w.n_copies, (int)blockIdx.x - tables, (int)gridDim.x - tables);
         return;
     }
     auto refer = [&](int p, int by) {
@@ -365,19 +378,23 @@ int copy_groups(const PageLayers &l, size_t most_copies) {
 
 }  // namespace
 
-hipError_t launch_pages_copy(const PageLayers &l, int n_pages, int n, const int32_t *src, const int32_t *dst, const int32_t *n_copies, hipStream_t s) {
+hipError_t launch_pages_copy(bool once, const PageLayers &l, int n_pages, int n, const int32_t *src, const int32_t *dst, const int32_t *n_copies, hipStream_t s) {
     const int groups = copy_groups(l, (size_t)n);
     if (groups <= 0) return hipSuccess;
-    hipLaunchKernelGGL(pages_copy_kernel, dim3(groups), dim3(kCopyThreads), 0, s, l, n_pages, src, dst, n_copies, n);
+    hipLaunchKernelGGL(once ? pages_copy_kernel<true> : pages_copy_kernel<false>, dim3(groups), dim3(kCopyThreads), 0, s, l, n_pages, src, dst, n_copies, n);
     return hipGetLastError();
 }
 
 hipError_t launch_pages_plan(int what, const PageTables &t, const PagesPlan &w, int n, const int32_t *xs, const int32_t *ys, int32_t *status, int32_t *new_page,
                              int32_t *n_live, hipStream_t s) {
     const dim3 one(1), block(kPlanThreads);
-    if (what == PAGES_FORK) hipLaunchKernelGGL(pages_plan_kernel<true>, one, block, 0, s, t, w, n, xs, ys, status);
-    else if (what == PAGES_RESIZE) hipLaunchKernelGGL(pages_plan_kernel<false>, one, block, 0, s, t, w, n, xs, ys, status);
-    else hipLaunchKernelGGL(pages_compact_plan_kernel, one, block, 0, s, t, w, new_page, n_live);
+    const bool far = t.n_pages > 4 * kScanNear * kPlanThreads;
+    if (what == PAGES_FORK)
+        hipLaunchKernelGGL((far ? pages_plan_kernel<true, kScanFar> : pages_plan_kernel<true, kScanNear>), one, block, 0, s, t, w, n, xs, ys, status);
+    else if (what == PAGES_RESIZE)
+        hipLaunchKernelGGL((far ? pages_plan_kernel<false, kScanFar> : pages_plan_kernel<false, kScanNear>), one, block, 0, s, t, w, n, xs, ys, status);
+    else
+        hipLaunchKernelGGL((far ? pages_compact_plan_kernel<kScanFar> : pages_compact_plan_kernel<kScanNear>), one, block, 0, s, t, w, new_page, n_live);
     return hipGetLastError();
 }
 

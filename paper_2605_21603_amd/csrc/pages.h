@@ -28,7 +28,8 @@ struct PagesPlan {
     int32_t *n_copies, *owner, *first, *had, *has, *need, *length, *src, *copy_src, *copy_dst, *fresh;
 };
 
-hipError_t launch_pages_copy(const PageLayers &l, int n_pages, int n, const int32_t *src, const int32_t *dst, const int32_t *n_copies, hipStream_t s);
+// once: no page is read twice.  n_copies (DEVICE), if given, says how many of the n pairs there are.
+hipError_t launch_pages_copy(bool once, const PageLayers &l, int n_pages, int n, const int32_t *src, const int32_t *dst, const int32_t *n_copies, hipStream_t s);
 hipError_t launch_pages_plan(int what, const PageTables &t, const PagesPlan &w, int n, const int32_t *xs, const int32_t *ys, int32_t *status, int32_t *new_page,
                              int32_t *n_live, hipStream_t s);
 // Tables and counts of n requests (compaction: rows), and the planned copies, at most most_copies of them.
