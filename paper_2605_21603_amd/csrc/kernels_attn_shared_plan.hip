@@ -61,15 +61,15 @@ __device__ __forceinline__ int item_positions(const PlanRule &rule, long long ow
 // the CU waits for its claim, its pages, its first tile and its stores: items where they are no more than that, and all by items where the batch's
 // would take the chip no longer than a block's 14 us.  `batch` = sub-tiles of shared keys over tokens.  General form: by items up to one set of columns.
 __device__ __forceinline__ bool by_items(const PlanRule &rule, long long batch, int tokens, int chunk) {
-    const long long sets = (tokens + rule.tg_few - 1) / rule.tg_few;
-    return rule.tiles ? sets <= 1 : batch * rule.n_kv < 13000 * rule.tg_few || 17 * sets * chunk < 10000 + 15 * chunk;
+    const int sets = (tokens + rule.tg_few - 1) / rule.tg_few;
+    return rule.tiles ? sets <= 1 : batch * rule.n_kv < 13000 * rule.tg_few || 17ll * sets * chunk < 10000 + 15 * chunk;
 }
 
 // Set bits from bit `at` on, as far as they follow one another.
-constexpr int kAhead = 4;                       // words behind a batch: rows that go on with its last one's run or sequence
-__device__ __forceinline__ int ones_from(const unsigned long long *words, int at) {
+constexpr int kAhead = 4;                       // words behind a round: rows that go on with its last one's run or sequence
+__device__ __forceinline__ int ones_from(const unsigned long long *words, int n_words, int at) {
     int n = 0;
-    for (int w = at >> 6, b = at & 63; w < 16 + kAhead; ++w, b = 0) {
+    for (int w = at >> 6, b = at & 63; w < n_words; ++w, b = 0) {
         const unsigned long long gap = ~(words[w] >> b);        // the shift brings in zeros: a gap at 64 - b at the latest, unless b is 0
         const int run = gap ? __ffsll(gap) - 1 : 64;
         n += run;
@@ -78,23 +78,26 @@ __device__ __forceinline__ int ones_from(const unsigned long long *words, int at
     return n;
 }
 
-// One workgroup of 16 waves, a thread per row and round of 1024 rows.
-template <bool SHARE>
-__global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *__restrict__ seq_of_token, const int32_t *__restrict__ pos_of_token, int rows,
+// One workgroup, a thread per row and round of WAVES * 64 rows.  Four waves, one to a SIMD, where there are few rows: an instruction that sixteen go through
+// takes four times as long.
+template <bool SHARE, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int32_t *__restrict__ seq_of_token, const int32_t *__restrict__ pos_of_token, int rows,
                                                                 AttnPrefix prefix, AttnShape sh, PlanRule rule, SharedPlan w) {
+    constexpr int ROUND = WAVES * 64;
+    static_assert(WAVES >= kAhead, "a wave per word of rows ahead");
     __shared__ int lead_of[SHARE ? kShareSeqs : 1], pages_of[SHARE ? kShareSeqs : 1], members[SHARE ? kShareSeqs : 1];
     __shared__ int batch[2], cost[2];                                // sub-tiles of shared and of own keys; what the lists take, in 1/16 us
-    __shared__ int edge_lead[17], edge_keys[17], edge_seq[17];       // the last row of each wave's 64, and of the round before
-    __shared__ unsigned long long p_goes_on[16 + kAhead], s_goes_on[16 + kAhead];      // rows like the one before them: the same prefix, the same sequence
-    __shared__ int sums[5][16];
+    __shared__ int edge_lead[WAVES + 1], edge_keys[WAVES + 1], edge_seq[WAVES + 1];       // the last row of each wave's 64, and of the round before
+    __shared__ unsigned long long p_goes_on[WAVES + kAhead], s_goes_on[WAVES + kAhead];      // rows like the one before them: the same prefix, the same sequence
+    __shared__ int sums[4][WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ps = sh.page_size, max_pages = sh.max_pages_per_seq;
     const bool any = SHARE && prefix.lead != nullptr;
     int next_seq = -1, next_pos = -1;                                // the next round's row, on its way
     if (tid < rows) { next_seq = seq_of_token[tid]; next_pos = pos_of_token[tid]; }
     if (tid < 2) batch[tid] = cost[tid] = 0;
-    if (tid < 17) edge_lead[tid] = edge_keys[tid] = edge_seq[tid] = -1;
+    if (tid <= WAVES) edge_lead[tid] = edge_keys[tid] = edge_seq[tid] = -1;
     if (any) {
-        for (int s = tid; s < prefix.n_seqs; s += 1024) {
+        for (int s = tid; s < prefix.n_seqs; s += ROUND) {
             const int lead = prefix.lead[s], pages = prefix.pages[s];
             const bool ok = lead >= 0 && lead < prefix.n_seqs && pages >= 1 && pages < max_pages;
             lead_of[s] = ok ? lead : -1;
@@ -102,11 +105,11 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
             members[s] = 0;
         }
         __syncthreads();
-        for (int s = tid; s < prefix.n_seqs; s += 1024)
+        for (int s = tid; s < prefix.n_seqs; s += ROUND)
             if (lead_of[s] >= 0) atomicAdd(&members[lead_of[s]], 1);
         __syncthreads();
         // from here on: the batch's tokens behind a prefix that two sequences and more name; -1: nobody shares with this lead
-        for (int s = tid; s < prefix.n_seqs; s += 1024) members[s] = members[s] > 1 ? 0 : -1;
+        for (int s = tid; s < prefix.n_seqs; s += ROUND) members[s] = members[s] > 1 ? 0 : -1;
     }
     __syncthreads();
     struct Row { int seq, pos, lead, keys; };                        // lead -1: shares nothing
@@ -120,7 +123,7 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
     };
     if constexpr (SHARE) {                                           // all rows of the batch, whichever of them are served here
         int shared = 0, own = 0;
-        for (int t = tid; t < prefix.rows; t += 1024) {
+        for (int t = tid; t < prefix.rows; t += ROUND) {
             const int seq = prefix.seq_of_token[t], before = prefix.seq_of_token[max(t - 1, 0)], after = prefix.seq_of_token[min(t + 1, prefix.rows - 1)];
             const Row r = row_of(seq, prefix.pos_of_token[t]);
             if (r.lead >= 0) {
@@ -141,16 +144,16 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
     const long long batch_shared = batch[0] / rule.tg_many, batch_own = batch[1];
     int run_before = -1, before[3] = {0, 0, 0};                      // the last run's first row; entries of items, p_blocks, s_blocks so far
     int cost_items = 0, cost_blocks = 0;
-    for (int t0 = 0; t0 < rows; t0 += 1024) {
+    for (int t0 = 0; t0 < rows; t0 += ROUND) {
         const int t = t0 + tid;
         const Row r = row_of(next_seq, next_pos);
         const bool on = r.lead >= 0, live = t < rows;
         const int s_seq = !live ? -2 : r.pos < 0 ? -3 - t : r.seq * max_pages + r.keys / ps, p = r.pos - r.keys;
         // rows behind this round that go on with its last one's run or sequence
         int ahead_seq = -1, ahead_pos = -1;
-        if (tid < 64 * kAhead && t0 + 1024 + tid < rows) { ahead_seq = seq_of_token[t0 + 1024 + tid]; ahead_pos = pos_of_token[t0 + 1024 + tid]; }
+        if (tid < 64 * kAhead && t0 + ROUND + tid < rows) { ahead_seq = seq_of_token[t0 + ROUND + tid]; ahead_pos = pos_of_token[t0 + ROUND + tid]; }
         next_seq = next_pos = -1;
-        if (t + 1024 < rows) { next_seq = seq_of_token[t + 1024]; next_pos = pos_of_token[t + 1024]; }
+        if (t + ROUND < rows) { next_seq = seq_of_token[t + ROUND]; next_pos = pos_of_token[t + ROUND]; }
         if (lane == 63) { edge_lead[wave + 1] = on ? r.lead : -1; edge_keys[wave + 1] = r.keys; edge_seq[wave + 1] = s_seq; }
         __syncthreads();
         int lead_before = __shfl_up(on ? r.lead : -1, 1, 64), keys_before = __shfl_up(r.keys, 1, 64), seq_before = __shfl_up(s_seq, 1, 64);
@@ -160,20 +163,20 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
         if (lane == 0) { p_goes_on[wave] = p_mask; s_goes_on[wave] = s_mask; }
         if (wave < kAhead) {
             const Row x = row_of(ahead_seq, ahead_pos);
-            const unsigned long long pm = __ballot(x.lead >= 0 && x.lead == edge_lead[16] && x.keys == edge_keys[16]);
-            const unsigned long long sm = __ballot(x.pos >= 0 && x.seq * max_pages + x.keys / ps == edge_seq[16]);
-            if (lane == 0) { p_goes_on[16 + wave] = pm; s_goes_on[16 + wave] = sm; }
+            const unsigned long long pm = __ballot(x.lead >= 0 && x.lead == edge_lead[WAVES] && x.keys == edge_keys[WAVES]);
+            const unsigned long long sm = __ballot(x.pos >= 0 && x.seq * max_pages + x.keys / ps == edge_seq[WAVES]);
+            if (lane == 0) { p_goes_on[WAVES + wave] = pm; s_goes_on[WAVES + wave] = sm; }
         }
         int run = scan_wave(on && !same_prefix ? t : -1, -1, [](int a, int b) { return a > b ? a : b; });          // the latest start up to here
-        if (lane == 63) sums[4][wave] = run;
+        if (lane == 63) sums[3][wave] = run;
         __syncthreads();
         run = max(run, run_before);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            if (k < wave) run = max(run, sums[4][k]);
-            run_before = max(run_before, sums[4][k]);
+        for (int k = 0; k < WAVES; ++k) {
+            if (k < wave) run = max(run, sums[3][k]);
+            run_before = max(run_before, sums[3][k]);
         }
-        if (tid == 0) { edge_lead[0] = edge_lead[16]; edge_keys[0] = edge_keys[16]; edge_seq[0] = edge_seq[16]; }   // (read again behind the next barriers)
+        if (tid == 0) { edge_lead[0] = edge_lead[WAVES]; edge_keys[0] = edge_keys[WAVES]; edge_seq[0] = edge_seq[WAVES]; }   // (read again behind the next barriers)
         int p_tok = 0, p_n = 0, p_ct = 64, s_tok = 0, s_n = 0, s_ct = 64;              // what row t leads: tokens and chunks
         bool few = false, single = false;
         if (on) {
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
         const bool leads = on && (t - run) % width == 0;
         if constexpr (SHARE) {
             if (leads) {
-                p_tok = min(width, 1 + ones_from(p_goes_on, tid + 1));
+                p_tok = min(width, 1 + ones_from(p_goes_on, WAVES + kAhead, tid + 1));
                 p_n = (r.keys - 1 + p_ct) / p_ct;
             }
             if (live && r.pos >= 0) {
@@ -193,7 +196,7 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
                 single = !same_seq && !(s_goes_on[(tid + 1) >> 6] >> ((tid + 1) & 63) & 1);
                 s_ct = single || rule.tiles ? item_positions(rule, batch_own, (p / tg + 1) * tg) : prefill_chunk_positions((p / tg + 1) * tg);
                 if (!same_seq || p % tg == 0) {
-                    s_tok = single ? 1 : min(tg - p % tg, 1 + ones_from(s_goes_on, tid + 1));    // rows of the sequence in its aligned block
+                    s_tok = single ? 1 : min(tg - p % tg, 1 + ones_from(s_goes_on, WAVES + kAhead, tid + 1));    // rows of the sequence in its aligned block
                     s_n = (p + s_tok - 1 + s_ct) / s_ct;                                          // chunks the last of them reaches
                 }
             }
@@ -215,7 +218,7 @@ __global__ __launch_bounds__(1024) void attn_shared_plan_kernel(const int32_t *_
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
+            for (int j = 0; j < WAVES; ++j) {
                 if (j < wave) start[k] += sums[k][j];
                 before[k] += sums[k][j];
             }
@@ -306,8 +309,9 @@ hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, c
     if (p.n_seqs > kShareSeqs) p.lead = nullptr;
     const PlanRule rule{form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG, TG, sh.chunk_pages * sh.page_size, sh.n_kv,
                         form == SHARE_TILES};
-    hipLaunchKernelGGL(form == SHARE_NOTHING ? attn_shared_plan_kernel<false> : attn_shared_plan_kernel<true>, dim3(1), dim3(1024), 0, s, seq_of_token, pos_of_token, rows, p,
-                       sh, rule, w);
+    const bool small = prefix.rows <= 256 && prefix.n_seqs <= 1024;       // (340 rows: 54 us in one round of 16 waves, 57 in two of 4)
+    const auto kernel = form == SHARE_NOTHING ? attn_shared_plan_kernel<false, 16> : small ? attn_shared_plan_kernel<true, 4> : attn_shared_plan_kernel<true, 16>;
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(form != SHARE_NOTHING && small ? 256 : 1024), 0, s, seq_of_token, pos_of_token, rows, p, sh, rule, w);
     return hipGetLastError();
 }
 
