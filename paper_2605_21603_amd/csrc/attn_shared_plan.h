@@ -14,7 +14,7 @@ struct SharedPlan {
     // per chunk.
     int32_t *p_seq, *p_pos, *p_ct, *s_seq, *s_pos, *s_ct;
     // Work lists, [0] = entries, entry i at 2 + 2 i: the first token row, then chunk | tokens << 20.  items: up to 16 columns (a token and a q head
-    // each) of shared keys, or a single token's own keys (kOwnItem set in the row).  p_blocks, s_blocks: query blocks of shared and
+    // each) of shared keys, or the own keys of a sequence's tokens (kOwnItem set in the row).  p_blocks, s_blocks: query blocks of shared and
     // of own keys.  [1] = a counter that entries are claimed from.
     int32_t *items, *p_blocks, *s_blocks;
     // What the lists take, in us of one CU and kv head: [0] the items, [1] the query blocks.

@@ -30,10 +30,12 @@ struct SharedArgs {
     prefill::SubTiles page;
 };
 
-// One wave's work: up to 16 columns (a token and a q head each) against one chunk of one kv head, all of them seeing all of it.
+// One wave's work: up to 16 columns (a token and a q head each) against one chunk of one kv head.  Shared keys all of them see; of own keys, each token
+// one more than the one before it.
 struct Item {
     int t, n_tok, own, c, g;              // first token row, tokens, whose keys, chunk, kv head
     int first, last, end;                 // the chunk's sub-tiles; the first position past it
+    int full;                             // the first position that its first token does not see
     const int32_t *table;
 };
 
@@ -68,13 +70,15 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
         m.own = row >> 30;
         m.c = packed & 0xfffff;
         m.n_tok = packed >> 20;
-        const int keys = (m.own ? a.plan.s_pos : a.plan.p_pos)[m.t] + 1;
+        const int keys = (m.own ? a.plan.s_pos : a.plan.p_pos)[m.t] + (m.own ? m.n_tok : 1);
         m.table = a.block_table + (m.own ? a.plan.s_seq : a.plan.p_seq)[m.t];
-        // chunks of equal size up to rounding, a function of the half's own length
-        const int subs = (keys + 15) >> 4, most = (m.own ? a.plan.s_ct : a.plan.p_ct)[m.t] >> 4, n = (subs + most - 1) / most, per = (subs + n - 1) / n;
+        // chunks of equal size up to rounding, a function of the half's own length; fixed ones where tokens of different lengths share them
+        const int subs = (keys + 15) >> 4, most = (m.own ? a.plan.s_ct : a.plan.p_ct)[m.t] >> 4, n = (subs + most - 1) / most;
+        const int per = m.own && m.n_tok > 1 ? most : (subs + n - 1) / n;
         m.first = m.c * per;
         m.last = min(m.first + per, subs) - 1;
         m.end = min(keys, (m.last + 1) * 16);
+        m.full = m.own ? min(m.end, keys - m.n_tok + 1) : m.end;
         return m;
     };
     u32x4 kr[2][TILE][4];
@@ -116,13 +120,15 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
             for (int ks = 0; ks < 4; ++ks) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[B][i][ks]), q[ks], s[i], 0, 0, 0);
             s[i] *= scale;
         }
-        if (at + 16 * TILE > m.end) {                                    // the chunk ends in this tile (wave-uniform)
+        // the chunk ends in this tile, or some token does not see all of it (wave-uniform)
+        if (at + 16 * TILE > m.full) {
+            const int seen = min(m.end, m.full + col_tok);               // by this lane's column
 #pragma unroll
             for (int i = 0; i < TILE; ++i) {
                 const int n = m.end - (at + 16 * i + 4 * lq);            // valid positions of this lane's four
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (r >= n) s[i][r] = -INFINITY;
+                    if (at + 16 * i + 4 * lq + r >= seen) s[i][r] = -INFINITY;
                 // what lies past them must not meet its zero probability (0 * NaN)
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
@@ -189,7 +195,7 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
         float l = l_run;
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
-        if (col_tok < cur.n_tok) {
+        if (col_tok < cur.n_tok && cur.full + col_tok > cur.first * 16) {    // (a token that ends before the chunk has no partial of it)
             const size_t at = part_index(sh, cur.t + col_tok, cur.g * G + col_head, cur.own ? a.shared_slots + cur.c : cur.c);
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4 *>(a.part_o + at * HD + dt * 16 + 4 * lq) = acc[dt];
@@ -280,9 +286,11 @@ __global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *_
                 if (i0 + j0) load(i0 + j0);
 #pragma unroll
                 for (int j = 0; j < LOADS; ++j) {
-                    const float wj = __shfl(wgt, j0 + j, 32);
+                    {
+                        const float wj = __shfl(wgt, j0 + j, 32);
 #pragma unroll
-                    for (int k = 0; k < SETS; ++k) acc[k] += v[j][k] * wj;
+                        for (int k = 0; k < SETS; ++k) acc[k] += v[j][k] * wj;
+                    }
                 }
             }
         }

@@ -36,19 +36,26 @@ __device__ __forceinline__ int sum_all(int x) { return __builtin_amdgcn_readlane
 
 struct PlanRule {
     int tg_many, tg_few;                // tokens of a query block and of an item
-    int most_positions;                 // the longest chunk of a single token's own keys
+    unsigned many_magic, few_magic;     // ceil(2^32 / .)
+    int short_tokens;                   // a sequence of no more tokens than this in the step is served by items: a set of columns, which waves anywhere take
+                                        // (64 of 2 to 8 tokens, 512 to 2048 keys of their own: 116 us with one alone, 112 so, 131 with up to two sets, which read their keys twice)
+    int most_positions;                 // the longest chunk of an item's own keys
     int n_kv;
     bool tiles;                         // SHARE_TILES
 };
 
 // Chunks, from the batch, in sub-tiles of 16 positions: `shared` = keys of a prefix times query blocks that attend it, summed over the
-// prefixes; `own` = keys of single tokens, summed.  A chunk costs a partial set per column, written and read again, and too few of them
+// prefixes; `own` = sequences' own keys, summed.  A chunk costs a partial set per column, written and read again, and too few of them
 // leave CUs idle.  Query blocks: what gives every CU (general form: one of four workgroups to a CU) a piece, or, beside single tokens' keys,
 // what takes half as long as those (a tile of 64 positions some 4 us, keys of one kv head 512 bytes at 5.5 TB/s); two tiles at least, and at most
 // 32 chunks a prefix.
+// All chunks of a prefix are then of one length, as a short last one would cost nearly all that a chunk does: as many as asked for (12 prompts of 33 to 300 tokens behind
+// 4096 keys: 202 -> 176 us), or, where query blocks have the chip to themselves, one fewer if that makes them at most half as long again (166 us; beside
+// items it delays the end, 256 tokens behind 4 prefixes 276 -> 295 us).
 __device__ __forceinline__ int block_positions(const PlanRule &rule, long long shared, long long own, int keys) {
     const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 16, own * rule.n_kv * 3 / 256), (long long)keys / 32);
-    return (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll);
+    const int ct = (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll), n = max((keys + (shared > 8 * own && !rule.tiles ? ct / 2 : ct - 1)) / ct, (keys + 8191) / 8192);
+    return ((keys + n - 1) / n + 63) / 64 * 64;
 }
 // Items: four rounds of the chip's 2048 waves (general form: two of 1024 workgroups), at least 64 (128) positions and at most 64 chunks a token.
 __device__ __forceinline__ int item_positions(const PlanRule &rule, long long own, int keys) {
@@ -65,6 +72,9 @@ __device__ __forceinline__ bool by_items(const PlanRule &rule, long long batch, 
     return rule.tiles ? sets <= 1 : batch * rule.n_kv < 13000 * rule.tg_few || 17ll * sets * chunk < 10000 + 15 * chunk;
 }
 
+// x / d by magic = ceil(2^32 / d), for d of at most 256 (0 for d = 1): exact below 2^24, and a division beyond.
+__device__ __forceinline__ int quotient(int x, int d, unsigned magic) { return magic && x < 1 << 24 ? (int)__umulhi((unsigned)x, magic) : x / d; }
+
 // Set bits from bit `at` on, as far as they follow one another.
 constexpr int kAhead = 4;                       // words behind a round: rows that go on with its last one's run or sequence
 __device__ __forceinline__ int ones_from(const unsigned long long *words, int n_words, int at) {
@@ -78,24 +88,27 @@ __device__ __forceinline__ int ones_from(const unsigned long long *words, int n_
     return n;
 }
 
+constexpr int kFewWaves = 4;
 // One workgroup, a thread per row and round of WAVES * 64 rows.  Four waves, one to a SIMD, where there are few rows: an instruction that sixteen go through
-// takes four times as long.
+// takes four times as long; those rows are one round, so nothing of them lies before or behind it.
 template <bool SHARE, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int32_t *__restrict__ seq_of_token, const int32_t *__restrict__ pos_of_token, int rows,
                                                                 AttnPrefix prefix, AttnShape sh, PlanRule rule, SharedPlan w) {
     constexpr int ROUND = WAVES * 64;
+    constexpr bool ONE = WAVES == kFewWaves;                         // rows <= ROUND
     static_assert(WAVES >= kAhead, "a wave per word of rows ahead");
-    __shared__ int lead_of[SHARE ? kShareSeqs : 1], pages_of[SHARE ? kShareSeqs : 1], members[SHARE ? kShareSeqs : 1];
+    // per sequence: its lead (-1: none), pages, whether items serve its shared keys (the sign) and their chunks; per lead: who shares
+    __shared__ int lead_of[SHARE ? kShareSeqs : 1], pages_of[SHARE ? kShareSeqs : 1], rule_of[SHARE && WAVES != kFewWaves ? kShareSeqs : 1], members[SHARE ? kShareSeqs : 1];
     __shared__ int batch[2], cost[2];                                // sub-tiles of shared and of own keys; what the lists take, in 1/16 us
-    __shared__ int edge_lead[WAVES + 1], edge_keys[WAVES + 1], edge_seq[WAVES + 1];       // the last row of each wave's 64, and of the round before
+    __shared__ int edge_lead[WAVES + 1], edge_keys[WAVES + 1], edge_seq[WAVES + 1], edge_shift[WAVES + 1];       // the last row of each wave's 64, and of the round before
     __shared__ unsigned long long p_goes_on[WAVES + kAhead], s_goes_on[WAVES + kAhead];      // rows like the one before them: the same prefix, the same sequence
-    __shared__ int sums[4][WAVES];
+    __shared__ int sums[5][WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ps = sh.page_size, max_pages = sh.max_pages_per_seq;
     const bool any = SHARE && prefix.lead != nullptr;
     int next_seq = -1, next_pos = -1;                                // the next round's row, on its way
     if (tid < rows) { next_seq = seq_of_token[tid]; next_pos = pos_of_token[tid]; }
     if (tid < 2) batch[tid] = cost[tid] = 0;
-    if (tid <= WAVES) edge_lead[tid] = edge_keys[tid] = edge_seq[tid] = -1;
+    if (tid <= WAVES) edge_lead[tid] = edge_keys[tid] = edge_seq[tid] = edge_shift[tid] = -1;
     if (any) {
         for (int s = tid; s < prefix.n_seqs; s += ROUND) {
             const int lead = prefix.lead[s], pages = prefix.pages[s];
@@ -112,26 +125,26 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         for (int s = tid; s < prefix.n_seqs; s += ROUND) members[s] = members[s] > 1 ? 0 : -1;
     }
     __syncthreads();
-    struct Row { int seq, pos, lead, keys; };                        // lead -1: shares nothing
+    struct Row { int seq, pos, lead, pages, keys; };                 // lead -1: shares nothing
     auto row_of = [&](int seq, int pos) {
-        Row r{seq, pos, -1, 0};
+        Row r{seq, pos, -1, 0, 0};
         if (any && pos >= 0 && seq >= 0 && seq < prefix.n_seqs && lead_of[seq] >= 0 && members[lead_of[seq]] >= 0 && pos >= pages_of[seq] * ps) {
             r.lead = lead_of[seq];
-            r.keys = pages_of[seq] * ps;
+            r.pages = pages_of[seq];
+            r.keys = r.pages * ps;
         }
         return r;
     };
     if constexpr (SHARE) {                                           // all rows of the batch, whichever of them are served here
         int shared = 0, own = 0;
         for (int t = tid; t < prefix.rows; t += ROUND) {
-            const int seq = prefix.seq_of_token[t], before = prefix.seq_of_token[max(t - 1, 0)], after = prefix.seq_of_token[min(t + 1, prefix.rows - 1)];
+            const int seq = prefix.seq_of_token[t], before = prefix.seq_of_token[max(t - 1, 0)];
             const Row r = row_of(seq, prefix.pos_of_token[t]);
             if (r.lead >= 0) {
                 atomicAdd(&members[r.lead], 1);
                 shared += r.keys >> 4;
             }
-            const bool first = t == 0 || before != seq, last = t + 1 == prefix.rows || after != seq;
-            if (rule.tiles ? first || (r.pos - r.keys) % rule.tg_many == 0 : first && last) own += (r.pos - r.keys + 16) >> 4;
+            if (t == 0 || before != seq || (rule.tiles && (r.pos - r.keys) % rule.tg_many == 0)) own += (r.pos - r.keys + 16) >> 4;
         }
         shared = sum_all(shared);
         own = sum_all(own);
@@ -142,61 +155,97 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         __syncthreads();
     }
     const long long batch_shared = batch[0] / rule.tg_many, batch_own = batch[1];
-    int run_before = -1, before[3] = {0, 0, 0};                      // the last run's first row; entries of items, p_blocks, s_blocks so far
+    auto prefix_rule = [&](int lead, int keys) {
+        const int ct = block_positions(rule, batch_shared, batch_own, keys);
+        return by_items(rule, batch[0], members[lead], ct) ? item_positions(rule, batch_own, 2 * keys) | (int)0x80000000u : ct;
+    };
+    if (any && !ONE) {                                               // (one round: every row for itself, and no barrier)
+        for (int s = tid; s < prefix.n_seqs; s += ROUND) {
+            const int lead = lead_of[s];
+            if (lead >= 0 && members[lead] >= 0) rule_of[s] = prefix_rule(lead, pages_of[s] * ps);
+        }
+        __syncthreads();
+    }
+    // a value per wave, joined: over the waves below this one, and over all
+    struct Joined { int below, all; };
+    auto over_waves = [&](const int *row, int empty, auto op) {
+        if constexpr (ONE) {
+            Joined j{empty, empty};
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) {
+                if (k < wave) j.below = op(j.below, row[k]);
+                j.all = op(j.all, row[k]);
+            }
+            return j;
+        }
+        const int x = scan_wave(lane < WAVES ? row[lane] : empty, empty, op), at = __builtin_amdgcn_readfirstlane(wave);
+        return Joined{at ? __builtin_amdgcn_readlane(x, at - 1) : empty, __builtin_amdgcn_readlane(x, 63)};
+    };
+    int run_before = -1, seq_before_run = -1, before[3] = {0, 0, 0}; // the last run's and sequence's first rows; entries of items, p_blocks, s_blocks so far
     int cost_items = 0, cost_blocks = 0;
     for (int t0 = 0; t0 < rows; t0 += ROUND) {
         const int t = t0 + tid;
         const Row r = row_of(next_seq, next_pos);
         const bool on = r.lead >= 0, live = t < rows;
-        const int s_seq = !live ? -2 : r.pos < 0 ? -3 - t : r.seq * max_pages + r.keys / ps, p = r.pos - r.keys;
+        const int s_seq = !live ? -2 : r.pos < 0 ? -3 - t : r.seq * max_pages + r.pages, p = r.pos - r.keys;
+        const int shift = p - t;                                     // the same where positions follow one another, as items and query blocks take them to
         // rows behind this round that go on with its last one's run or sequence
         int ahead_seq = -1, ahead_pos = -1;
-        if (tid < 64 * kAhead && t0 + ROUND + tid < rows) { ahead_seq = seq_of_token[t0 + ROUND + tid]; ahead_pos = pos_of_token[t0 + ROUND + tid]; }
+        if (!ONE && tid < 64 * kAhead && t0 + ROUND + tid < rows) { ahead_seq = seq_of_token[t0 + ROUND + tid]; ahead_pos = pos_of_token[t0 + ROUND + tid]; }
         next_seq = next_pos = -1;
-        if (t + ROUND < rows) { next_seq = seq_of_token[t + ROUND]; next_pos = pos_of_token[t + ROUND]; }
-        if (lane == 63) { edge_lead[wave + 1] = on ? r.lead : -1; edge_keys[wave + 1] = r.keys; edge_seq[wave + 1] = s_seq; }
+        if (!ONE && t + ROUND < rows) { next_seq = seq_of_token[t + ROUND]; next_pos = pos_of_token[t + ROUND]; }
+        if (lane == 63) { edge_lead[wave + 1] = on ? r.lead : -1; edge_keys[wave + 1] = r.keys; edge_seq[wave + 1] = s_seq; edge_shift[wave + 1] = shift; }
         __syncthreads();
-        int lead_before = __shfl_up(on ? r.lead : -1, 1, 64), keys_before = __shfl_up(r.keys, 1, 64), seq_before = __shfl_up(s_seq, 1, 64);
-        if (lane == 0) { lead_before = edge_lead[wave]; keys_before = edge_keys[wave]; seq_before = edge_seq[wave]; }
-        const bool same_prefix = on && lead_before == r.lead && keys_before == r.keys, same_seq = live && seq_before == s_seq;
+        int lead_before = __shfl_up(on ? r.lead : -1, 1, 64), keys_before = __shfl_up(r.keys, 1, 64), seq_before = __shfl_up(s_seq, 1, 64), shift_before = __shfl_up(shift, 1, 64);
+        if (lane == 0) { lead_before = edge_lead[wave]; keys_before = edge_keys[wave]; seq_before = edge_seq[wave]; shift_before = edge_shift[wave]; }
+        const bool same_prefix = on && lead_before == r.lead && keys_before == r.keys, same_seq = live && seq_before == s_seq && shift_before == shift;
         const unsigned long long p_mask = __ballot(same_prefix), s_mask = __ballot(same_seq);
         if (lane == 0) { p_goes_on[wave] = p_mask; s_goes_on[wave] = s_mask; }
-        if (wave < kAhead) {
+        if constexpr (ONE) {
+            if (tid < kAhead) p_goes_on[WAVES + tid] = s_goes_on[WAVES + tid] = 0;
+        } else if (wave < kAhead) {
             const Row x = row_of(ahead_seq, ahead_pos);
             const unsigned long long pm = __ballot(x.lead >= 0 && x.lead == edge_lead[WAVES] && x.keys == edge_keys[WAVES]);
-            const unsigned long long sm = __ballot(x.pos >= 0 && x.seq * max_pages + x.keys / ps == edge_seq[WAVES]);
+            const unsigned long long sm = __ballot(x.pos >= 0 && x.seq * max_pages + x.pages == edge_seq[WAVES] && x.pos - x.keys - (t0 + ROUND + tid) == edge_shift[WAVES]);
             if (lane == 0) { p_goes_on[WAVES + wave] = pm; s_goes_on[WAVES + wave] = sm; }
         }
-        int run = scan_wave(on && !same_prefix ? t : -1, -1, [](int a, int b) { return a > b ? a : b; });          // the latest start up to here
-        if (lane == 63) sums[3][wave] = run;
+        const auto later = [](int a, int b) { return a > b ? a : b; };
+        int run = scan_wave(on && !same_prefix ? t : -1, -1, later), s_run = scan_wave(!same_seq ? t : -1, -1, later);          // the latest starts up to here
+        if (lane == 63) { sums[3][wave] = run; sums[4][wave] = s_run; }
         __syncthreads();
         run = max(run, run_before);
-#pragma unroll
-        for (int k = 0; k < WAVES; ++k) {
-            if (k < wave) run = max(run, sums[3][k]);
-            run_before = max(run_before, sums[3][k]);
-        }
-        if (tid == 0) { edge_lead[0] = edge_lead[WAVES]; edge_keys[0] = edge_keys[WAVES]; edge_seq[0] = edge_seq[WAVES]; }   // (read again behind the next barriers)
+        s_run = max(s_run, seq_before_run);
+        const auto [run_below, run_all] = over_waves(sums[3], -1, later);
+        const auto [s_below, s_all] = over_waves(sums[4], -1, later);
+        run = max(run, run_below);
+        s_run = max(s_run, s_below);
+        run_before = max(run_before, run_all);
+        seq_before_run = max(seq_before_run, s_all);
+        if (!ONE && tid == 0) { edge_lead[0] = edge_lead[WAVES]; edge_keys[0] = edge_keys[WAVES]; edge_seq[0] = edge_seq[WAVES]; edge_shift[0] = edge_shift[WAVES]; }   // (read again behind the next barriers)
         int p_tok = 0, p_n = 0, p_ct = 64, s_tok = 0, s_n = 0, s_ct = 64;              // what row t leads: tokens and chunks
         bool few = false, single = false;
         if (on) {
-            p_ct = block_positions(rule, batch_shared, batch_own, r.keys);
-            few = by_items(rule, batch[0], members[r.lead], p_ct);
-            if (few) p_ct = item_positions(rule, batch_own, 2 * r.keys);
+            const int r_rule = ONE ? prefix_rule(r.lead, r.keys) : rule_of[r.seq];
+            few = r_rule < 0;
+            p_ct = r_rule & 0x7fffffff;
         }
         const int width = few ? rule.tg_few : rule.tg_many;
-        const bool leads = on && (t - run) % width == 0;
+        const bool leads = on && t - run == quotient(t - run, width, few ? rule.few_magic : rule.many_magic) * width;
         if constexpr (SHARE) {
             if (leads) {
                 p_tok = min(width, 1 + ones_from(p_goes_on, WAVES + kAhead, tid + 1));
                 p_n = (r.keys - 1 + p_ct) / p_ct;
             }
             if (live && r.pos >= 0) {
-                const int tg = rule.tg_many;
-                single = !same_seq && !(s_goes_on[(tid + 1) >> 6] >> ((tid + 1) & 63) & 1);
-                s_ct = single || rule.tiles ? item_positions(rule, batch_own, (p / tg + 1) * tg) : prefill_chunk_positions((p / tg + 1) * tg);
-                if (!same_seq || p % tg == 0) {
-                    s_tok = single ? 1 : min(tg - p % tg, 1 + ones_from(s_goes_on, WAVES + kAhead, tid + 1));    // rows of the sequence in its aligned block
+                const int tg = rule.tg_many, block = quotient(p, tg, rule.many_magic);
+                const bool alone = !same_seq && !(s_goes_on[(tid + 1) >> 6] >> ((tid + 1) & 63) & 1);
+                int behind = 0;                                                                   // rows of the sequence behind this one, if they are few
+                if (!alone && t - s_run < rule.short_tokens) behind = ones_from(s_goes_on, WAVES + kAhead, tid + 1);
+                single = alone || t - s_run + 1 + behind <= rule.short_tokens;
+                s_ct = single ? item_positions(rule, batch_own, p + behind + 1) : rule.tiles ? item_positions(rule, batch_own, (block + 1) * tg) : prefill_chunk_positions((block + 1) * tg);
+                const int at = single ? t - s_run - quotient(t - s_run, rule.tg_few, rule.few_magic) * rule.tg_few : same_seq ? p - block * tg : 0;
+                if (at == 0) {                                                                     // rows of the sequence in this item, or in its aligned block
+                    s_tok = single ? min(rule.tg_few, behind + 1) : min(tg - (p - block * tg), 1 + ones_from(s_goes_on, WAVES + kAhead, tid + 1));
                     s_n = (p + s_tok - 1 + s_ct) / s_ct;                                          // chunks the last of them reaches
                 }
             }
@@ -217,11 +266,9 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
-#pragma unroll
-            for (int j = 0; j < WAVES; ++j) {
-                if (j < wave) start[k] += sums[k][j];
-                before[k] += sums[k][j];
-            }
+            const auto [below, all] = over_waves(sums[k], 0, [](int a, int b) { return a + b; });
+            start[k] += below;
+            before[k] += all;
         }
         if (live) {
             w.s_seq[t] = r.pos < 0 ? -1 : s_seq;
@@ -237,6 +284,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
                 for (int c = 0; c < s_n; ++c) { *at++ = single ? t | kOwnItem : t; *at++ = c | (s_tok << 20); }
             }
         }
+        if (ONE) break;
         __syncthreads();
     }
     if constexpr (SHARE) {
@@ -307,11 +355,12 @@ hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, c
     const int G = sh.n_q / sh.n_kv, TG = G <= 16 ? 16 / G : 1;
     AttnPrefix p = prefix;
     if (p.n_seqs > kShareSeqs) p.lead = nullptr;
-    const PlanRule rule{form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG, TG, sh.chunk_pages * sh.page_size, sh.n_kv,
-                        form == SHARE_TILES};
-    const bool small = prefix.rows <= 256 && prefix.n_seqs <= 1024;       // (340 rows: 54 us in one round of 16 waves, 57 in two of 4)
-    const auto kernel = form == SHARE_NOTHING ? attn_shared_plan_kernel<false, 16> : small ? attn_shared_plan_kernel<true, 4> : attn_shared_plan_kernel<true, 16>;
-    hipLaunchKernelGGL(kernel, dim3(1), dim3(form != SHARE_NOTHING && small ? 256 : 1024), 0, s, seq_of_token, pos_of_token, rows, p, sh, rule, w);
+    const int many = form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG;
+    auto magic = [](int d) { return (unsigned)((0x100000000ull + d - 1) / d); };
+    const PlanRule rule{many, TG, magic(many), magic(TG), form == SHARE_LISTS ? TG : 1, sh.chunk_pages * sh.page_size, sh.n_kv, form == SHARE_TILES};
+    const bool small = std::max(rows, prefix.rows) <= kFewWaves * 64 && prefix.n_seqs <= 1024;       // (340 rows: 54 us in one round of 16 waves, 57 in two of 4)
+    const auto kernel = form == SHARE_NOTHING ? attn_shared_plan_kernel<false, 16> : small ? attn_shared_plan_kernel<true, kFewWaves> : attn_shared_plan_kernel<true, 16>;
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(form != SHARE_NOTHING && small ? kFewWaves * 64 : 1024), 0, s, seq_of_token, pos_of_token, rows, p, sh, rule, w);
     return hipGetLastError();
 }
 

@@ -159,6 +159,30 @@ def test_several_tokens_a_sequence(shape):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("shape", ["fast", "fast_g3", "fast_g1", "fast_g16", "fast_p48", "bf16_64", "f32_64"])
+@pytest.mark.parametrize("new", [2, 3, 4, 5, 17])
+def test_drafts_behind_long_keys_of_their_own(shape, new):
+    """Few tokens a sequence: their own keys end inside a tile, a chunk or a page, each token's one further."""
+    owns = [new, new + 1, 15 + new, 16, 64, 64 + new, 65, 129, 500 + new, 1024, 1030]
+    c = Case(shape, group("a", 6, [max(o, new) for o in owns], new=new) + [(None, 0, 900, new, 1), (None, 0, new, new), ("a", 6, 800, 1)])
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("shape", ["fast", "fast_g3", "bf16_64", "f32_64", "odd_page"])
+def test_positions_that_repeat_or_skip(shape):
+    """Rows of one sequence that do not follow one another each attend the keys up to their own position; the last page of the
+    table's last row is full, so one key more would be read past it."""
+    ps = SHAPES[shape][3]
+    own = 6 * ps
+    c = Case(shape, group("a", 4, [own, own, own], new=6) + [(None, 0, own, 3), ("a", 4, own, 30)], spare=0)
+    at = 0
+    for s, pos in enumerate([[-1, -1, -1, -1, -1, -1], [-6, -4, -4, -4, -2, -1], [-9, -8, -3, -3, -2, -2], [-7, -7, -1], [-30 + i // 2 for i in range(30)]]):
+        c.pos[at:at + len(pos)] = c.ctx[s] + np.array(pos)
+        at += len(pos)
+    c.args["pos_of_token"].copy_(torch.from_numpy(c.pos))
+    c.check(c.run())
+
+
 @pytest.mark.parametrize("shape,shared", [("fast", 300), ("fast", 531), ("fast_p48", 111), ("bf16_64", 150), ("f32_64", 70)])
 @pytest.mark.parametrize("n", [2, 7, 9, 40])
 def test_long_prefixes(shape, shared, n):
