@@ -53,14 +53,14 @@ struct PlanRule {
 // 4096 keys: 202 -> 176 us), or, where query blocks have the chip to themselves, one fewer if that makes them at most half as long again (166 us; beside
 // items it delays the end, 256 tokens behind 4 prefixes 276 -> 295 us).
 __device__ __forceinline__ int block_positions(const PlanRule &rule, long long shared, long long own, int keys) {
-    const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 16, own * rule.n_kv * 3 / 256), (long long)keys / 32);
+    const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 16, own * rule.n_kv * 3 / 256), ((long long)keys + 31) / 32);
     const int ct = (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll), n = max((keys + (shared > 8 * own && !rule.tiles ? ct / 2 : ct - 1)) / ct, (keys + 8191) / 8192);
     return ((keys + n - 1) / n + 63) / 64 * 64;
 }
 // Items: four rounds of the chip's 2048 waves (general form: two of 1024 workgroups), at least 64 (128) positions and at most 64 chunks a token.
 __device__ __forceinline__ int item_positions(const PlanRule &rule, long long own, int keys) {
     const long long want = own * rule.n_kv / (rule.tiles ? 128 : 512), least = rule.tiles ? 128 : 64;
-    return (int)max(min(max((want + 63) / 64 * 64, least), (long long)rule.most_positions), ((long long)keys / 64 + 63) / 64 * 64);
+    return (int)max(min(max((want + 63) / 64 * 64, least), (long long)rule.most_positions), ((long long)keys + 4095) / 4096 * 64);
 }
 
 // Whether a prefix that `tokens` tokens attend is served by items, which read K and V once for every tg_few of them, and not by query blocks, which read

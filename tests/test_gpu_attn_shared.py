@@ -183,6 +183,23 @@ def test_positions_that_repeat_or_skip(shape):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("shape,keys", [("fast", 4096), ("fast", 4097), ("fast", 4159), ("fast", 8255), ("fast_p48", 4100), ("bf16_64", 8193), ("f32_64", 8200)])
+@pytest.mark.parametrize("new", [1, 3])
+def test_lengths_just_past_what_the_most_chunks_hold(shape, keys, new):
+    """As many chunks as a token has partials for: neither the rows around it nor what lies behind the partials is written."""
+    c = Case(shape, [(None, 0, 9, 1), (None, 0, keys, new), (None, 0, 17, 1), (None, 0, keys, new)])
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("shape,shared", [("fast", 256), ("fast", 257), ("fast", 4097), ("fast_p48", 86), ("bf16_64", 257)])
+@pytest.mark.parametrize("n", [3, 90])
+def test_prefixes_just_past_what_the_most_chunks_hold(shape, shared, n):
+    if n > 3 and shared > 1000:
+        n = 20
+    c = Case(shape, group("a", shared, [3] * n) + [(None, 0, 5, 1)])
+    c.check(c.run())
+
+
 @pytest.mark.parametrize("shape,shared", [("fast", 300), ("fast", 531), ("fast_p48", 111), ("bf16_64", 150), ("f32_64", 70)])
 @pytest.mark.parametrize("n", [2, 7, 9, 40])
 def test_long_prefixes(shape, shared, n):
