@@ -567,12 +567,25 @@ def _stream_of(stream: Optional[torch.cuda.Stream], device) -> C.c_void_p:
     return C.c_void_p(stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index))
 
 
+def _launch(device, call) -> None:
+    """The call with `device` current: a launch on another device's stream is an error."""
+    if torch._C._cuda_getDevice() == device.index:
+        return _check(call())
+    with torch.cuda.device(device):
+        _check(call())
+
+
 def _int32(t: torch.Tensor, name: str, device, shape) -> int:
     """Device pointer of a contiguous int32 tensor of that shape on that device."""
     if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
         raise ValueError("%s: a contiguous int32 tensor of shape %s on %s, not %s %s on %s" %
                          (name, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
+
+
+def _on_gpu(device) -> None:
+    if device.type != "cuda":
+        raise ValueError("tensors on a GPU, not on %s" % device)
 
 
 def _cache_pair(k: torch.Tensor, v: torch.Tensor):
@@ -616,6 +629,7 @@ class SharedAttention:
                                     ints(pos_of_token, "pos_of_token", T), _int32(block_table, "block_table", self.device, (n_seqs, width)), width,
                                     ints(prefix_lead, "prefix_lead", n_seqs), ints(prefix_pages, "prefix_pages", n_seqs),
                                     k_cache.data_ptr(), v_cache.data_ptr(), None, 0)
+        _on_gpu(self.device)
         nbytes = lib().dyn_attn_shared_workspace_bytes(C.byref(self.batch))
         if nbytes == 0 and T:
             raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error())
@@ -627,7 +641,7 @@ class SharedAttention:
 
     def forward(self, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Writes and returns `out`; on `stream`, by default torch's current one."""
-        _check(lib().dyn_attn_shared(C.byref(self.batch), _stream_of(stream, self.device)))
+        _launch(self.device, lambda: lib().dyn_attn_shared(C.byref(self.batch), _stream_of(stream, self.device)))
         return self.out
 
 
@@ -654,6 +668,7 @@ class PagePool:
                                   C.cast(self._ptrs[0], C.c_void_p), C.cast(self._ptrs[1], C.c_void_p),
                                   _int32(block_table, "block_table", self.device, (rows, width)), _int32(seq_len, "seq_len", self.device, (rows,)),
                                   _int32(ref_count, "ref_count", self.device, (n_pages,)), None, 0)
+        _on_gpu(self.device)
         nbytes = lib().dyn_pages_workspace_bytes(C.byref(self.pool), self.max_requests)
         if nbytes == 0:
             raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error() or "max_requests = %d" % self.max_requests)
@@ -664,15 +679,15 @@ class PagePool:
     def copy(self, src: torch.Tensor, dst: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Pages src[i] to dst[i], in every layer."""
         n = len(src)
-        _check(lib().dyn_pages_copy(C.byref(self.pool), n, _int32(src, "src", self.device, (n,)), _int32(dst, "dst", self.device, (n,)),
-                                    _stream_of(stream, self.device)))
+        pairs = _int32(src, "src", self.device, (n,)), _int32(dst, "dst", self.device, (n,))
+        _launch(self.device, lambda: lib().dyn_pages_copy(C.byref(self.pool), n, *pairs, _stream_of(stream, self.device)))
 
     def _requests(self, call, a, b, names, status, stream) -> torch.Tensor:
         n = len(a)
         if status is None:
             status = torch.empty(n, dtype=torch.int32, device=self.device)
-        _check(call(C.byref(self.pool), n, _int32(a, names[0], self.device, (n,)), _int32(b, names[1], self.device, (n,)),
-                    _int32(status, "status", self.device, (n,)), _stream_of(stream, self.device)))
+        args = [_int32(t, name, self.device, (n,)) for t, name in ((a, names[0]), (b, names[1]), (status, "status"))]
+        _launch(self.device, lambda: call(C.byref(self.pool), n, *args, _stream_of(stream, self.device)))
         return status
 
     def fork(self, parent: torch.Tensor, child: torch.Tensor, status: Optional[torch.Tensor] = None,
@@ -690,6 +705,6 @@ class PagePool:
         n = self.pool.n_pages
         new_page = torch.empty(n, dtype=torch.int32, device=self.device) if new_page is None else new_page
         n_live = torch.empty(1, dtype=torch.int32, device=self.device) if n_live is None else n_live
-        _check(lib().dyn_pages_compact(C.byref(self.pool), _int32(new_page, "new_page", self.device, (n,)), _int32(n_live, "n_live", self.device, (1,)),
-                                       _stream_of(stream, self.device)))
+        args = _int32(new_page, "new_page", self.device, (n,)), _int32(n_live, "n_live", self.device, (1,))
+        _launch(self.device, lambda: lib().dyn_pages_compact(C.byref(self.pool), *args, _stream_of(stream, self.device)))
         return new_page, n_live

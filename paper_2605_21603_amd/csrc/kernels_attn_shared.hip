@@ -356,11 +356,14 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
     part.max_chunks = sh.max_chunks + prefix.max_chunks;
     if (form == SHARE_LISTS) {
         const auto kernel = sh.page_size == 16 ? attn_shared_kernel<false> : attn_shared_kernel<true>;
-        static std::atomic<bool> attr_set[2];
-        if (!attr_set[sh.page_size != 16]) {
+        static std::atomic<unsigned long long> attr_set[2];               // a bit per device
+        int device = 0;
+        if ((e = hipGetDevice(&device)) != hipSuccess) return e;
+        const unsigned long long bit = 1ull << (device & 63);
+        if (!(attr_set[sh.page_size != 16] & bit)) {
             e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, prefill::lds_bytes());
             if (e != hipSuccess) return e;
-            attr_set[sh.page_size != 16] = true;
+            attr_set[sh.page_size != 16] |= bit;
         }
         const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, ld_q, prefix.max_chunks, part_o,
                            part_ml, prefill::SubTiles{sh.page_size / 16, (unsigned)((0x100000000ull + sh.page_size / 16 - 1) / (sh.page_size / 16))}};

@@ -72,6 +72,8 @@ def test_binding_checks_tensors():
                 dict(q=torch.zeros(1, 4, 32).expand(3, 4, 32))):
         with pytest.raises(ValueError):
             B.SharedAttention(**dict(ok, **bad))
+    with pytest.raises(ValueError, match="on a GPU"):
+        B.SharedAttention(**ok)
 
 
 def layer_and_batch(name="c2_small", **fields):

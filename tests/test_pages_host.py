@@ -91,6 +91,8 @@ def test_binding_checks_tensors():
         args = dict(dict(k_cache=cache, v_cache=cache, block_table=table, seq_len=lens, ref_count=ref, max_requests=2), **bad)
         with pytest.raises(ValueError):
             B.PagePool(**args)
+    with pytest.raises(ValueError, match="on a GPU"):
+        B.PagePool(cache, cache, table, lens, ref, 2)
 
 
 def test_the_model_keeps_counts_in_step_with_rows():
