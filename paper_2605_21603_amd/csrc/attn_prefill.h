@@ -72,6 +72,7 @@ struct SubTiles {
     unsigned magic;                    // ceil(2^32 / per)
     __device__ __forceinline__ int page_of(int sub) const { return (int)__umulhi((unsigned)sub, magic); }     // exact for sub * per below 2^32
 };
+
 template <bool PARTS = false, bool WIDE_PAGES = false>
 __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qkv,
                                                               const int32_t *__restrict__ seq_of_token,
@@ -82,7 +83,8 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                                                               bf16_t *__restrict__ out, int ld_out,
                                                               float *__restrict__ part_o, float *__restrict__ part_ml,
                                                               AttnShape sh, const int32_t *__restrict__ plan, int32_t *__restrict__ counter,
-                                                              const int32_t *__restrict__ ct_of_token, int ld_q = 0, SubTiles page = SubTiles{}) {
+                                                              const int32_t *__restrict__ ct_of_token, int ld_q = 0, SubTiles page = SubTiles{},
+                                                              int32_t *odd = nullptr) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int32_t *pid = reinterpret_cast<int32_t *>(lds + kRing * kTile);      // physical pages of the chunk
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -143,6 +145,24 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
         // keys its first token attends; columns of dead tokens or heads carry zeros and are never stored
         const int wave_min_keys = wave_tok0 < n_tok ? pos_of_token[t0 + wave_tok0] + 1 : 0;
         __syncthreads();                                                  // pid is visible
+        // PARTS: values behind the block's first token, which some columns must not see: *odd is set if they are not all finite
+        if constexpr (PARTS) {
+            const int late0 = max(pos_of_token[t0] + 1, lp0 * PS), late1 = min(n_keys, (lp0 + n_pg) * PS), per = WIDE_PAGES ? page.per : 1;
+            const int most = late0 < late1 ? ((late1 + PS - 1) / PS - late0 / PS) * 256 : 0;
+#pragma clang loop unroll(disable)
+            for (int i = tid; i < most; i += kWaves * 64) {
+                const int sub = late0 / PS + (i >> 8), slot = WIDE_PAGES ? sub - page.page_of(sub) * per : 0, r = i >> 1 & 127, h = i & 1;
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(v_cache + ((size_t)pid[sub - lp0] * sh.n_kv + g) * (PS * HD) * per + r * PS * per + slot * PS + h * 8);
+                bool found = false;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int at = sub * PS + h * 8 + 2 * d;
+                    found |= at >= late0 && at < late1 && (x[d] & 0x7f80u) == 0x7f80u;
+                    found |= at + 1 >= late0 && at + 1 < late1 && (x[d] & 0x7f800000u) == 0x7f800000u;
+                }
+                if (found) *odd = 1;
+            }
+        }
 
         // Wave w copies one 4 KB page of every tile: K pages 0..3 (waves 0..3), V pages 0..3 (waves 4..7).
         const int wpage = wave & (kTP - 1);

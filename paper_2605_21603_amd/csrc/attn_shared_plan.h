@@ -19,6 +19,7 @@ struct SharedPlan {
     int32_t *items, *p_blocks, *s_blocks;
     // What the lists take, in us of one CU and kv head: [0] the items, [1] the query blocks.
     float *cost;
+    int32_t *odd;                      // set where some of the values that only later tokens of a sequence see are infinities or NaN
 };
 constexpr int kOwnItem = 1 << 30;
 

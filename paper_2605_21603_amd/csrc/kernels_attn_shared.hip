@@ -39,6 +39,31 @@ struct Item {
     const int32_t *table;
 };
 
+// Whether one of two bf16, at positions `first` and first + 1, lies at `full` or behind it and is an infinity or NaN.
+__device__ __forceinline__ bool late_odd(uint32_t x, int first, int full) {
+    return (first >= full && (x & 0x7f80u) == 0x7f80u) || (first + 1 >= full && (x & 0x7f800000u) == 0x7f800000u);
+}
+
+__device__ __forceinline__ Item fetch_item(const SharedArgs &a, int i) {
+    Item m;
+    const int e = i / a.sh.n_kv, row = a.plan.items[2 + 2 * e], packed = a.plan.items[3 + 2 * e];
+    m.g = i - e * a.sh.n_kv;
+    m.t = row & (kOwnItem - 1);
+    m.own = row >> 30;
+    m.c = packed & 0xfffff;
+    m.n_tok = packed >> 20;
+    const int keys = (m.own ? a.plan.s_pos : a.plan.p_pos)[m.t] + (m.own ? m.n_tok : 1);
+    m.table = a.block_table + (m.own ? a.plan.s_seq : a.plan.p_seq)[m.t];
+    // chunks of equal size up to rounding, a function of the half's own length; fixed ones where tokens of different lengths share them
+    const int subs = (keys + 15) >> 4, most = (m.own ? a.plan.s_ct : a.plan.p_ct)[m.t] >> 4, n = (subs + most - 1) / most;
+    const int per = m.own && m.n_tok > 1 ? most : (subs + n - 1) / n;
+    m.first = m.c * per;
+    m.last = min(m.first + per, subs) - 1;
+    m.end = min(keys, (m.last + 1) * 16);
+    m.full = m.own ? min(m.end, keys - m.n_tok + 1) : m.end;
+    return m;
+}
+
 // The items: every n_blocks-th from `block` on is this workgroup's, and its waves take them as they come, from a counter in LDS.  (A fixed share
 // to every wave: of the two waves of a SIMD the older gets its loads first, and with equal shares - 256 tokens of 1024 keys - the older ones were through
 // after 149 us and the others after 196.)  K and V go from memory straight into MFMA operand layout,
@@ -62,25 +87,7 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
     int item = take();
     if (item >= n_items) return;
 
-    auto fetch = [&](int i) {
-        Item m;
-        const int e = i / sh.n_kv, row = a.plan.items[2 + 2 * e], packed = a.plan.items[3 + 2 * e];
-        m.g = i - e * sh.n_kv;
-        m.t = row & (kOwnItem - 1);
-        m.own = row >> 30;
-        m.c = packed & 0xfffff;
-        m.n_tok = packed >> 20;
-        const int keys = (m.own ? a.plan.s_pos : a.plan.p_pos)[m.t] + (m.own ? m.n_tok : 1);
-        m.table = a.block_table + (m.own ? a.plan.s_seq : a.plan.p_seq)[m.t];
-        // chunks of equal size up to rounding, a function of the half's own length; fixed ones where tokens of different lengths share them
-        const int subs = (keys + 15) >> 4, most = (m.own ? a.plan.s_ct : a.plan.p_ct)[m.t] >> 4, n = (subs + most - 1) / most;
-        const int per = m.own && m.n_tok > 1 ? most : (subs + n - 1) / n;
-        m.first = m.c * per;
-        m.last = min(m.first + per, subs) - 1;
-        m.end = min(keys, (m.last + 1) * 16);
-        m.full = m.own ? min(m.end, keys - m.n_tok + 1) : m.end;
-        return m;
-    };
+    auto fetch = [&](int i) { return fetch_item(a, i); };
     u32x4 kr[2][TILE][4];
     u32x2 vr[2][TILE][8];
     bf16x8 q[4], q_next[4];
@@ -134,6 +141,14 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
                 for (int dt = 0; dt < 8; ++dt) {
                     vr[B][i][dt][0] &= (n > 0 ? 0x0000ffffu : 0u) | (n > 1 ? 0xffff0000u : 0u);
                     vr[B][i][dt][1] &= (n > 2 ? 0x0000ffffu : 0u) | (n > 3 ? 0xffff0000u : 0u);
+                }
+                if (m.full < m.end) {
+                    bool found = false;
+#pragma unroll
+                    for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) found |= late_odd(vr[B][i][dt][h], at + 16 * i + 4 * lq + 2 * h, m.full);
+                    if (found) *a.plan.odd = 1;
                 }
             }
         }
@@ -230,20 +245,69 @@ __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(Sh
         int32_t *const list = own ? w.s_blocks : w.p_blocks;
         if (list[0] == 0) continue;
         prefill::attn_prefill_items<true, WIDE_PAGES>(a.q, own ? w.s_seq : w.p_seq, own ? w.s_pos : w.p_pos, a.block_table, a.k, a.v, nullptr, 0,
-                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q, a.page);
+                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q, a.page, w.odd);
     }
+}
+
+// What the merge needs to attend a row's own keys again.
+struct MendArgs {
+    const bf16_t *q, *k, *v;
+    const int32_t *block_table, *s_seq, *odd;
+    int ld_q;
+};
+
+// Positions first .. end - 1 for one column (q: its 128 values), by a half-wave: a position to a lane for the scores, four head-dim indices for the values, and
+// nothing read behind `end`.
+__device__ __forceinline__ void attend_plain(const MendArgs &a, const bf16_t *q, const int32_t *table, int n_kv, int g, int ps, int first, int end, float *po, float *pml) {
+    const int sub = threadIdx.x & 31;
+    const float scale = 1.4426950408889634f / sqrtf((float)HD);
+    float top = -INFINITY, l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto place = [&](int j, int &slot) {
+        const int at = j / ps;
+        slot = j - at * ps;
+        return (size_t)table[at] * n_kv + g;
+    };
+#pragma clang loop unroll(disable)
+    for (int j0 = first; j0 < end; j0 += 32) {
+        const int n = min(32, end - j0);
+        int slot;
+        const size_t page = place(j0 + min(sub, n - 1), slot);
+        const bf16_t *kp = a.k + (page * ps + slot) * HD;
+        float s = 0.f;
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < HD; ++i) s += bf2f(q[i]) * bf2f(kp[i]);
+        s = sub < n ? s * scale : -INFINITY;
+        float now = fmaxf(top, s);
+        for (int off = 16; off >= 1; off >>= 1) now = fmaxf(now, __shfl_xor(now, off, 32));
+        const float ref = now == -INFINITY ? 0.f : now, alpha = exp2f(top - ref), p = exp2f(s - ref);
+        top = now;
+        l = l * alpha + p;
+        o *= alpha;
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < n; ++i) {
+            const float pi = __shfl(p, i, 32);
+            const bf16_t *vp = a.v + (place(j0 + i, slot) * HD + 4 * sub) * ps + slot;
+            o += pi * f32x4{bf2f(vp[0]), bf2f(vp[ps]), bf2f(vp[2 * ps]), bf2f(vp[3 * ps])};
+        }
+    }
+    for (int off = 16; off >= 1; off >>= 1) l += __shfl_xor(l, off, 32);
+    *reinterpret_cast<f32x4 *>(po + 4 * sub) = o;
+    if (sub == 0) { pml[0] = top; pml[1] = l; }
 }
 
 // Merge of a row's partials, shared chunks first, in order; four head-dim indices to a lane, two sets of them in the WIDE form (head dims above
 // 128).  Where there are rows to fill the chip a half-wave merges a (token, q head); else (SPLIT) a workgroup does, its eight half-waves every
 // eighth chunk each and the eight results in order through LDS.  A row without keys is zero.  What it costs is two dependent loads, of the row's chunk counts and
 // of its partials, so the first of those are all on their way beside the maxima and sums that weigh them.
-template <typename T, bool BASE2, bool WIDE, bool SPLIT>
-__global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
+// MEND: where the launch before found values that are not finite among those of later tokens than some column's, these met the column's zero probabilities
+// (0 * NaN), so all own keys are attended again, plainly, in that launch's chunks.
+template <typename T, bool BASE2, bool WIDE, bool SPLIT, bool MEND>
+__global__ __launch_bounds__(256) void attn_shared_combine_kernel(float *part_o, float *part_ml,
                                                                   const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
                                                                   const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct,
                                                                   int shared_slots, T *__restrict__ out, int ld_out, AttnShape sh,
-                                                                  int32_t *__restrict__ counter0, int32_t *__restrict__ counter1) {
+                                                                  int32_t *__restrict__ counter0, int32_t *__restrict__ counter1, MendArgs mend) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     constexpr int SETS = WIDE ? 2 : 1, LOADS = 16 / SETS / (SPLIT ? 2 : 1), STEP = SPLIT ? 8 : 1;
     // the lists' query blocks have all been claimed: from the start again for the next layer
@@ -264,6 +328,18 @@ __global__ __launch_bounds__(256) void attn_shared_combine_kernel(const float *_
             const int c = c0 + i * STEP;
             return first + (size_t)(c < n_shared ? c : shared_slots + c - n_shared) * next;
         };
+        if constexpr (MEND) {
+            if (*mend.odd) {
+#pragma clang loop unroll(disable)
+                for (int i = 0; i < count; ++i) {
+                    const int c = c0 + i * STEP - n_shared, g = h / (sh.n_q / sh.n_kv);
+                    if (c >= 0)
+                        attend_plain(mend, mend.q + (size_t)t * mend.ld_q + h * HD, mend.block_table + mend.s_seq[t], sh.n_kv, g, sh.page_size, c * sc, min((c + 1) * sc, sp + 1),
+                                     part_o + at(i) * HD, part_ml + at(i) * 2);
+                }
+                __threadfence_block();
+            }
+        }
         auto ml_of = [&](int i) { return i < count ? *reinterpret_cast<const f32x2 *>(part_ml + at(i) * 2) : f32x2{-INFINITY, 0.f}; };
         f32x4 v[LOADS][SETS];
         auto load = [&](int i0) {
@@ -383,19 +459,23 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
     // which of the two depends on the batch, so that a row's bits do not depend on the dispatch it is in
     const bool split = (long)prefix.rows * sh.n_q <= 512;
     const dim3 grid(rows, split ? sh.n_q : (sh.n_q + 7) / 8), block(256);
-#define DYN_COMBINE_AS(T, B2, WIDE, SPLIT)                                                                                                                  \
-    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE, SPLIT>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,              \
-                       prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, lists ? w.s_blocks + 1 : nullptr)
-#define DYN_COMBINE(T, B2)                                                                                      \
-    do {                                                                                                        \
-        if (split) {                                                                                            \
-            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, true); else DYN_COMBINE_AS(T, B2, false, true);   \
-        } else {                                                                                                \
-            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, false); else DYN_COMBINE_AS(T, B2, false, false); \
-        }                                                                                                       \
+    const MendArgs mend{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w.s_seq, w.odd, ld_q};
+#define DYN_COMBINE_AS(T, B2, WIDE, SPLIT, MEND)                                                                                                            \
+    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE, SPLIT, MEND>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,        \
+                       prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, lists ? w.s_blocks + 1 : nullptr, mend)
+#define DYN_COMBINE(T, B2)                                                                                                    \
+    do {                                                                                                                      \
+        if (split) {                                                                                                          \
+            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, true, false); else DYN_COMBINE_AS(T, B2, false, true, false);   \
+        } else {                                                                                                              \
+            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, false, false); else DYN_COMBINE_AS(T, B2, false, false, false); \
+        }                                                                                                                     \
     } while (0)
-    if (dtype == 0) DYN_COMBINE(float, false);
-    else if (form != SHARE_NOTHING) DYN_COMBINE(bf16_t, true);
+    if (lists) {
+        if (split) DYN_COMBINE_AS(bf16_t, true, false, true, true);
+        else DYN_COMBINE_AS(bf16_t, true, false, false, true);
+    } else if (dtype == 0) DYN_COMBINE(float, false);
+    else if (form == SHARE_TILES) DYN_COMBINE(bf16_t, true);
     else DYN_COMBINE(bf16_t, false);
 #undef DYN_COMBINE
 #undef DYN_COMBINE_AS
