@@ -57,9 +57,9 @@ __device__ __forceinline__ int block_positions(const PlanRule &rule, long long s
     const int ct = (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll), n = max((keys + (shared > 8 * own && !rule.tiles ? ct / 2 : ct - 1)) / ct, (keys + 8191) / 8192);
     return ((keys + n - 1) / n + 63) / 64 * 64;
 }
-// Items: four rounds of the chip's 2048 waves (general form: two of 1024 workgroups), at least 64 (128) positions and at most 64 chunks a token.
+// Items: four rounds of the chip's 2048 waves (general form: one of 1024 workgroups), at least 64 (128) positions and at most 64 chunks a token.
 __device__ __forceinline__ int item_positions(const PlanRule &rule, long long own, int keys) {
-    const long long want = own * rule.n_kv / (rule.tiles ? 128 : 512), least = rule.tiles ? 128 : 64;
+    const long long want = own * rule.n_kv / (rule.tiles ? 64 : 512), least = rule.tiles ? 128 : 64;
     return (int)max(min(max((want + 63) / 64 * 64, least), (long long)rule.most_positions), ((long long)keys + 4095) / 4096 * 64);
 }
 
