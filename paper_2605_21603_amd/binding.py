@@ -567,12 +567,7 @@ def _stream_of(stream: Optional[torch.cuda.Stream], device) -> C.c_void_p:
     return C.c_void_p(stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index))
 
 
-def _launch(device, call) -> None:
-    """The call with `device` current: a launch on another device's stream is an error."""
-    if torch._C._cuda_getDevice() == device.index:
-        return _check(call())
-    with torch.cuda.device(device):
-        _check(call())
+_current_device = torch._C._cuda_getDevice
 
 
 def _int32(t: torch.Tensor, name: str, device, shape) -> int:
@@ -641,7 +636,10 @@ class SharedAttention:
 
     def forward(self, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Writes and returns `out`; on `stream`, by default torch's current one."""
-        _launch(self.device, lambda: lib().dyn_attn_shared(C.byref(self.batch), _stream_of(stream, self.device)))
+        if _current_device() != self.device.index:                    # a launch on another device's stream is an error
+            with torch.cuda.device(self.device):
+                return self.forward(stream)
+        _check(lib().dyn_attn_shared(C.byref(self.batch), _stream_of(stream, self.device)))
         return self.out
 
 
@@ -678,16 +676,22 @@ class PagePool:
 
     def copy(self, src: torch.Tensor, dst: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Pages src[i] to dst[i], in every layer."""
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self.copy(src, dst, stream)
         n = len(src)
-        pairs = _int32(src, "src", self.device, (n,)), _int32(dst, "dst", self.device, (n,))
-        _launch(self.device, lambda: lib().dyn_pages_copy(C.byref(self.pool), n, *pairs, _stream_of(stream, self.device)))
+        _check(lib().dyn_pages_copy(C.byref(self.pool), n, _int32(src, "src", self.device, (n,)), _int32(dst, "dst", self.device, (n,)),
+                                    _stream_of(stream, self.device)))
 
     def _requests(self, call, a, b, names, status, stream) -> torch.Tensor:
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self._requests(call, a, b, names, status, stream)
         n = len(a)
         if status is None:
             status = torch.empty(n, dtype=torch.int32, device=self.device)
-        args = [_int32(t, name, self.device, (n,)) for t, name in ((a, names[0]), (b, names[1]), (status, "status"))]
-        _launch(self.device, lambda: call(C.byref(self.pool), n, *args, _stream_of(stream, self.device)))
+        _check(call(C.byref(self.pool), n, _int32(a, names[0], self.device, (n,)), _int32(b, names[1], self.device, (n,)),
+                    _int32(status, "status", self.device, (n,)), _stream_of(stream, self.device)))
         return status
 
     def fork(self, parent: torch.Tensor, child: torch.Tensor, status: Optional[torch.Tensor] = None,
@@ -702,9 +706,12 @@ class PagePool:
 
     def compact(self, new_page: Optional[torch.Tensor] = None, n_live: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
         """Moves the pages in use to the front; returns (where each page is now, -1 if it was free; how many are in use)."""
+        if _current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                return self.compact(new_page, n_live, stream)
         n = self.pool.n_pages
         new_page = torch.empty(n, dtype=torch.int32, device=self.device) if new_page is None else new_page
         n_live = torch.empty(1, dtype=torch.int32, device=self.device) if n_live is None else n_live
-        args = _int32(new_page, "new_page", self.device, (n,)), _int32(n_live, "n_live", self.device, (1,))
-        _launch(self.device, lambda: lib().dyn_pages_compact(C.byref(self.pool), *args, _stream_of(stream, self.device)))
+        _check(lib().dyn_pages_compact(C.byref(self.pool), _int32(new_page, "new_page", self.device, (n,)), _int32(n_live, "n_live", self.device, (1,)),
+                                       _stream_of(stream, self.device)))
         return new_page, n_live
