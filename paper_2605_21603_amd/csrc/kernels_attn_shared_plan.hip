@@ -40,26 +40,29 @@ struct PlanRule {
     int short_tokens;                   // a sequence of no more tokens than this in the step is served by items: a set of columns, which waves anywhere take
                                         // (64 of 2 to 8 tokens, 512 to 2048 keys of their own: 116 us with one alone, 112 so, 131 with up to two sets, which read their keys twice)
     int most_positions;                 // the longest chunk of an item's own keys
+    int least, least_long;              // the shortest chunk of an item; and where there are two rounds of such
     int n_kv;
     bool tiles;                         // SHARE_TILES
 };
 
 // Chunks, from the batch, in sub-tiles of 16 positions: `shared` = keys of a prefix times query blocks that attend it, summed over the
 // prefixes; `own` = sequences' own keys, summed.  A chunk costs a partial set per column, written and read again, and too few of them
-// leave CUs idle.  Query blocks: what gives every CU (general form: one of four workgroups to a CU) a piece, or, beside single tokens' keys,
-// what takes half as long as those (a tile of 64 positions some 4 us, keys of one kv head 512 bytes at 5.5 TB/s); two tiles at least, and at most
-// 32 chunks a prefix.
+// leave CUs idle.  Query blocks: what gives every CU (general form: one of four workgroups to a CU) a piece, or, beside items, what takes as long as those (a tile
+// of 64 positions some 2 us, keys of one kv head 512 bytes at 5 TB/s; in a third and a half of that, 64 tokens behind 2048 positions took 65 and 59 us and now take 60,
+// 256 behind 4 prefixes 275, 272 and 267, 64 of 4 drafts 97, 75 and 76, 256 of them 200, 192 and 187); two tiles at least, and at most 32 chunks a prefix.
 // All chunks of a prefix are then of one length, as a short last one would cost nearly all that a chunk does: as many as asked for (12 prompts of 33 to 300 tokens behind
 // 4096 keys: 202 -> 176 us), or, where query blocks have the chip to themselves, one fewer if that makes them at most half as long again (166 us; beside
 // items it delays the end, 256 tokens behind 4 prefixes 276 -> 295 us).
 __device__ __forceinline__ int block_positions(const PlanRule &rule, long long shared, long long own, int keys) {
-    const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 16, own * rule.n_kv * 3 / 256), ((long long)keys + 31) / 32);
+    const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 16, own * rule.n_kv * 3 / 64), ((long long)keys + 31) / 32);
     const int ct = (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll), n = max((keys + (shared > 8 * own && !rule.tiles ? ct / 2 : ct - 1)) / ct, (keys + 8191) / 8192);
     return ((keys + n - 1) / n + 63) / 64 * 64;
 }
-// Items: four rounds of the chip's 2048 waves (general form: one of 1024 workgroups), at least 64 (128) positions and at most 64 chunks a token.
+// Items: four rounds of the chip's 2048 waves (general form: one of 1024 workgroups), at least 64 positions, or 128 where those are two rounds (64 tokens of 16 to 1024
+// keys of their own beside 8 alone: 50.0 -> 47.5 us; but pages of 64 positions, 192 tokens of 3 to 584 keys: 98.5 -> 102.5, so 64 there; general form: 128), and at
+// most 64 chunks a token.
 __device__ __forceinline__ int item_positions(const PlanRule &rule, long long own, int keys) {
-    const long long want = own * rule.n_kv / (rule.tiles ? 64 : 512), least = rule.tiles ? 128 : 64;
+    const long long want = own * rule.n_kv / (rule.tiles ? 64 : 512), least = own * rule.n_kv >= 16384 ? rule.least_long : rule.least;
     return (int)max(min(max((want + 63) / 64 * 64, least), (long long)rule.most_positions), ((long long)keys + 4095) / 4096 * 64);
 }
 
@@ -249,11 +252,11 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
                     s_n = (p + s_tok - 1 + s_ct) / s_ct;                                          // chunks the last of them reaches
                 }
             }
-            // a position of an item 512 bytes at 19.5 GB/s; a query block's tile of 64 positions 1 us and up to 1 more where all its columns are live, a block and
-            // chunk 10 us around its tiles
+            // a position of an item 512 bytes at 19.5 GB/s; beside items, a query block's tile of 64 positions 2 us and up to 1 more where all its columns are live, a
+            // block and chunk 20 us around its tiles
             const int p_subs = p_n ? r.keys >> 4 : 0, s_subs = s_n ? (p + s_tok + 15) >> 4 : 0;
             cost_items += 7 * ((few ? p_subs : 0) + (single ? s_subs : 0));
-            cost_blocks += (few ? 0 : p_subs * 4 + p_subs * 4 / rule.tg_many * p_tok + p_n * 160) + (single ? 0 : s_subs * 4 + s_subs * 4 / rule.tg_many * s_tok + s_n * 160);
+            cost_blocks += (few ? 0 : p_subs * 8 + p_subs * 4 / rule.tg_many * p_tok + p_n * 320) + (single ? 0 : s_subs * 8 + s_subs * 4 / rule.tg_many * s_tok + s_n * 320);
         }
         const int mine[3] = {(few ? p_n : 0) + (single ? s_n : 0), few ? 0 : p_n, single ? 0 : s_n};
         int start[3];
@@ -359,7 +362,8 @@ hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, c
     if (p.n_seqs > kShareSeqs) p.lead = nullptr;
     const int many = form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG;
     auto magic = [](int d) { return (unsigned)((0x100000000ull + d - 1) / d); };
-    const PlanRule rule{many, TG, magic(many), magic(TG), form == SHARE_LISTS ? TG : 1, sh.chunk_pages * sh.page_size, sh.n_kv, form == SHARE_TILES};
+    const PlanRule rule{many, TG, magic(many), magic(TG), form == SHARE_LISTS ? TG : 1, sh.chunk_pages * sh.page_size, form == SHARE_TILES ? 128 : 64,
+                        form == SHARE_TILES || sh.page_size == 16 ? 128 : 64, sh.n_kv, form == SHARE_TILES};
     const bool small = std::max(rows, prefix.rows) <= kFewWaves * 64 && prefix.n_seqs <= 1024;       // (340 rows: 54 us in one round of 16 waves, 57 in two of 4)
     const auto kernel = form == SHARE_NOTHING ? attn_shared_plan_kernel<false, 16> : small ? attn_shared_plan_kernel<true, kFewWaves> : attn_shared_plan_kernel<true, 16>;
     hipLaunchKernelGGL(kernel, dim3(1), dim3(form != SHARE_NOTHING && small ? kFewWaves * 64 : 1024), 0, s, seq_of_token, pos_of_token, rows, p, sh, rule, w);
