@@ -3,7 +3,9 @@
 // A page is free while nothing names it (its reference count is 0).  Which pages a call takes is decided by one workgroup -
 // the lowest free ones, in the order of the requests, so that the answer does not depend on how the launch is scheduled -
 // and carried out by a second launch over the whole chip, which writes tables and counts and copies pages in every layer.  Between
-// the two nothing waits on the host.  Counts change by integer atomics: their order does not show.
+// the two nothing waits on the host.  Counts change by integer atomics: their order does not show.  Small calls are two launches' latency (a fork into 7, 32
+// layers: 5.3 + 5.5 us; growing and freeing those 4.8 + 3.2), large ones a copy (64 into 4, 8 layers, 155 MB: 6.1 + 31; 1593 of 4000 pages moved together, 975 MB: 5.0 + 187,
+// 5.2 TB/s).
 #include <algorithm>
 
 #include "common.h"
