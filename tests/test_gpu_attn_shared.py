@@ -10,6 +10,7 @@ from paper_2605_21603_amd import binding as B
 from workloads import gen
 
 from gpu_util import GpuRun, check_against_oracle, say
+from test_gpu_parity import cu_masks_halves
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -304,6 +305,55 @@ def test_more_rows_than_the_plan_looks_at_in_one_round():
         c.check(got)
 
 
+@pytest.mark.parametrize("rows", [255, 256, 257, 1023, 1024, 1025])
+def test_rows_around_the_plans_rounds(rows):
+    """As many rows as one round of the plan holds, one fewer and one more; a draft and a query block lie across the border."""
+    head = group("a", 2, [3] * (rows - 40)) + [("a", 2, 37, 37)]
+    c = Case("fast", head + [("b", 1, 9, 3), ("b", 1, 5, 1)] if rows > 1000 else head + group("b", 1, [9, 5, 7]))
+    got = c.run()
+    keep = np.zeros(len(c.seq), bool)
+    keep[::29] = keep[-50:] = True
+    got[torch.from_numpy(~keep).to(DEV)] = 0
+    c.pos[~keep] = -1
+    c.check(got)
+
+
+@pytest.mark.parametrize("n_seqs", [1024, 1025])
+def test_few_rows_of_many_sequences(n_seqs):
+    """The plan of few rows counts up to 1024 sequences' leads; a batch may have many more sequences than rows."""
+    c = Case("fast", group("a", 3, [5, 40, 7]) + group("b", 1, [1, 2]) + [(None, 0, 1, 0)] * (n_seqs - 5))
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("shape", ["bf16_256", "f32_128", "bf16_64", "narrow", "fast"])
+@pytest.mark.parametrize("copies", [1, 60])
+def test_merges_by_a_half_wave_and_by_a_workgroup(shape, copies):
+    """Few rows and many, one chunk a row to as many as there are."""
+    c = Case(shape, group("a", 24, [1, 700, 30] * copies) + [(None, 0, 3, 1), (None, 0, 3000, 1)])
+    got = c.run()
+    keep = np.zeros(len(c.seq), bool)
+    keep[::17] = keep[-3:] = True
+    got[torch.from_numpy(~keep).to(DEV)] = 0
+    c.pos[~keep] = -1
+    c.check(got)
+
+
+@pytest.mark.parametrize("shape", ["fast", "fast_p48", "bf16_64", "f32_32"])
+def test_offsets_beyond_32_bits(shape):
+    """A pool whose last pages lie beyond 2^32 bytes and 2^31 elements: the same bits as with these pages at the front."""
+    c = Case(shape, group("a", 7, [5, 300, 33]) + group("a", 7, [90, 20], new=15) + [(None, 0, 100, 1)])
+    want = c.run()
+    used = c.k.shape[0]
+    n = (1 << 31) // c.k[0].numel() + used + 7
+    for name in ("k", "v"):
+        small = getattr(c, name)
+        big = torch.zeros((n,) + small.shape[1:], device=DEV, dtype=small.dtype)
+        big[n - used:] = small
+        setattr(c, name, big)
+    c.args["block_table"] += n - used
+    assert torch.equal(c.run(), want)
+
+
 def test_captured_call_follows_the_arrays_and_two_graphs_share_a_workspace():
     a, b = Case("fast", group("a", 20, [3, 50, 17, 90, 4, 33, 61, 2, 9, 12, 14])), Case("fast", group("a", 9, [30, 5, 7]) + [(None, 0, 90, 1)], seed=1)
     atts = [c.attention() for c in (a, b)]
@@ -414,6 +464,20 @@ def test_layer_with_shared_prefixes(name, prefixes):
     got = forward(run, data, prefix, B.sequential(), noalloc=True)
     for a, b in zip(got, (y, k, v)):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@pytest.mark.parametrize("name,prefixes", [LAYERS[0], LAYERS[2], LAYERS[6]])
+def test_layer_with_shared_prefixes_on_partitions(name, prefixes):
+    """Micro-batches, or all attention, on half of the CUs: the same bits."""
+    prefixes = {f: (n, [s for s in members if gen.config(name).seqs[s][1] - gen.config(name).seqs[s][0] >= n * gen.config(name).shape.page_size]) for f, (n, members) in prefixes.items()}
+    w, data, prefix = shared_step(name, prefixes)
+    run = GpuRun(w, data)
+    want = forward(run, data, prefix, B.sequential())
+    k = len(w.nano_rows) - 1
+    for sched in (B.nano_schedule(w.nano_rows, stagger=1, partitions=[1 + i % 2 for i in range(k)], cu_masks=cu_masks_halves()),
+                  B.nano_schedule(w.nano_rows, stagger=2, partitions=[2] * k, op_partitions={B.DYN_OP_ATTN: 1}, cu_masks=cu_masks_halves())):
+        for a, b in zip(forward(run, data, prefix, sched), want):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
 def test_graphs_with_and_without_prefixes_are_not_taken_for_one_another():
