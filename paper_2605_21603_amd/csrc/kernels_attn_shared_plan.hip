@@ -78,19 +78,7 @@ __device__ __forceinline__ bool by_items(const PlanRule &rule, long long batch, 
 // x / d by magic = ceil(2^32 / d), for d of at most 256 (0 for d = 1): exact below 2^24, and a division beyond.
 __device__ __forceinline__ int quotient(int x, int d, unsigned magic) { return magic && x < 1 << 24 ? (int)__umulhi((unsigned)x, magic) : x / d; }
 
-// Set bits from bit `at` on, as far as they follow one another.
 constexpr int kAhead = 4;                       // words behind a round: rows that go on with its last one's run or sequence
-__device__ __forceinline__ int ones_from(const unsigned long long *words, int n_words, int at) {
-    int n = 0;
-    for (int w = at >> 6, b = at & 63; w < n_words; ++w, b = 0) {
-        const unsigned long long gap = ~(words[w] >> b);        // the shift brings in zeros: a gap at 64 - b at the latest, unless b is 0
-        const int run = gap ? __ffsll(gap) - 1 : 64;
-        n += run;
-        if (run < 64 - b) break;
-    }
-    return n;
-}
-
 constexpr int kFewWaves = 4;
 // One workgroup, a thread per row and round of WAVES * 64 rows.  Four waves, one to a SIMD, where there are few rows: an instruction that sixteen go through
 // takes four times as long; those rows are one round, so nothing of them lies before or behind it.
@@ -105,7 +93,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
     __shared__ int batch[2], cost[2];                                // sub-tiles of shared and of own keys; what the lists take, in 1/16 us
     __shared__ int edge_lead[WAVES + 1], edge_keys[WAVES + 1], edge_seq[WAVES + 1], edge_shift[WAVES + 1];       // the last row of each wave's 64, and of the round before
     __shared__ unsigned long long p_goes_on[WAVES + kAhead], s_goes_on[WAVES + kAhead];      // rows like the one before them: the same prefix, the same sequence
-    __shared__ int sums[5][WAVES];
+    __shared__ int sums[3][WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ps = sh.page_size, max_pages = sh.max_pages_per_seq;
     const bool any = SHARE && prefix.lead != nullptr;
     int next_seq = -1, next_pos = -1;                                // the next round's row, on its way
@@ -184,6 +172,24 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         const int x = scan_wave(lane < WAVES ? row[lane] : empty, empty, op), at = __builtin_amdgcn_readfirstlane(wave);
         return Joined{at ? __builtin_amdgcn_readlane(x, at - 1) : empty, __builtin_amdgcn_readlane(x, 63)};
     };
+    // The run that this thread's row lies in, of rows that each go on like the one before (a bit each; mine: this wave's): its first row, and how many of it are
+    // behind this row, up to kAhead words past the round.  before: the first row of the run that the round's last row lies in.
+    struct Run { int start, behind; };
+    auto run_of = [&](const unsigned long long *words, unsigned long long mine, int t0, int &before) {
+        const int at = __builtin_amdgcn_readfirstlane(wave);
+        const unsigned long long x = lane < (ONE ? WAVES : WAVES + kAhead) ? words[lane] : 0ull;
+        const int ones = x == ~0ull ? 64 : __ffsll(~x) - 1, last = 63 - __clzll((long long)~x);         // rows in front that go on, the last that does not
+        const unsigned long long cut = __ballot(x != ~0ull), below = cut & ((1ull << at) - 1), all = cut & ((1ull << WAVES) - 1);
+        const int next = __ffsll(cut >> (at + 1)) + at, beyond = (next - at - 1) * 64 + __builtin_amdgcn_readlane(ones, next);
+        auto start_in = [&](unsigned long long words_cut) {
+            const int k = __builtin_amdgcn_readfirstlane(63 - __clzll((long long)words_cut));
+            return t0 + k * 64 + __builtin_amdgcn_readlane(last, k);
+        };
+        const unsigned long long own = ~mine & ((2ull << lane) - 1), rest = ~(lane == 63 ? 0ull : mine >> (lane + 1));
+        const int start = below ? start_in(below) : before, run = __ffsll(rest) - 1;
+        if (all) before = start_in(all);
+        return Run{own ? t0 + at * 64 + 63 - __clzll((long long)own) : start, run < 63 - lane ? run : 63 - lane + beyond};
+    };
     int run_before = -1, seq_before_run = -1, before[3] = {0, 0, 0}; // the last run's and sequence's first rows; entries of items, p_blocks, s_blocks so far
     int cost_items = 0, cost_blocks = 0;
     for (int t0 = 0; t0 < rows; t0 += ROUND) {
@@ -204,26 +210,14 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         const bool same_prefix = on && lead_before == r.lead && keys_before == r.keys, same_seq = live && seq_before == s_seq && shift_before == shift;
         const unsigned long long p_mask = __ballot(same_prefix), s_mask = __ballot(same_seq);
         if (lane == 0) { p_goes_on[wave] = p_mask; s_goes_on[wave] = s_mask; }
-        if constexpr (ONE) {
-            if (tid < kAhead) p_goes_on[WAVES + tid] = s_goes_on[WAVES + tid] = 0;
-        } else if (wave < kAhead) {
+        if (!ONE && wave < kAhead) {
             const Row x = row_of(ahead_seq, ahead_pos);
             const unsigned long long pm = __ballot(x.lead >= 0 && x.lead == edge_lead[WAVES] && x.keys == edge_keys[WAVES]);
             const unsigned long long sm = __ballot(x.pos >= 0 && x.seq * max_pages + x.pages == edge_seq[WAVES] && x.pos - x.keys - (t0 + ROUND + tid) == edge_shift[WAVES]);
             if (lane == 0) { p_goes_on[WAVES + wave] = pm; s_goes_on[WAVES + wave] = sm; }
         }
-        const auto later = [](int a, int b) { return a > b ? a : b; };
-        int run = scan_wave(on && !same_prefix ? t : -1, -1, later), s_run = scan_wave(!same_seq ? t : -1, -1, later);          // the latest starts up to here
-        if (lane == 63) { sums[3][wave] = run; sums[4][wave] = s_run; }
         __syncthreads();
-        run = max(run, run_before);
-        s_run = max(s_run, seq_before_run);
-        const auto [run_below, run_all] = over_waves(sums[3], -1, later);
-        const auto [s_below, s_all] = over_waves(sums[4], -1, later);
-        run = max(run, run_below);
-        s_run = max(s_run, s_below);
-        run_before = max(run_before, run_all);
-        seq_before_run = max(seq_before_run, s_all);
+        const Run p_run = run_of(p_goes_on, p_mask, t0, run_before), s_run = run_of(s_goes_on, s_mask, t0, seq_before_run);
         if (!ONE && tid == 0) { edge_lead[0] = edge_lead[WAVES]; edge_keys[0] = edge_keys[WAVES]; edge_seq[0] = edge_seq[WAVES]; edge_shift[0] = edge_shift[WAVES]; }   // (read again behind the next barriers)
         int p_tok = 0, p_n = 0, p_ct = 64, s_tok = 0, s_n = 0, s_ct = 64;              // what row t leads: tokens and chunks
         bool few = false, single = false;
@@ -233,22 +227,20 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
             p_ct = r_rule & 0x7fffffff;
         }
         const int width = few ? rule.tg_few : rule.tg_many;
-        const bool leads = on && t - run == quotient(t - run, width, few ? rule.few_magic : rule.many_magic) * width;
+        const int p_at = t - p_run.start, s_at = t - s_run.start;
+        const bool leads = on && p_at == quotient(p_at, width, few ? rule.few_magic : rule.many_magic) * width;
         if constexpr (SHARE) {
             if (leads) {
-                p_tok = min(width, 1 + ones_from(p_goes_on, WAVES + kAhead, tid + 1));
+                p_tok = min(width, 1 + p_run.behind);
                 p_n = (r.keys - 1 + p_ct) / p_ct;
             }
             if (live && r.pos >= 0) {
                 const int tg = rule.tg_many, block = quotient(p, tg, rule.many_magic);
-                const bool alone = !same_seq && !(s_goes_on[(tid + 1) >> 6] >> ((tid + 1) & 63) & 1);
-                int behind = 0;                                                                   // rows of the sequence behind this one, if they are few
-                if (!alone && t - s_run < rule.short_tokens) behind = ones_from(s_goes_on, WAVES + kAhead, tid + 1);
-                single = alone || t - s_run + 1 + behind <= rule.short_tokens;
-                s_ct = single ? item_positions(rule, batch_own, p + behind + 1) : rule.tiles ? item_positions(rule, batch_own, (block + 1) * tg) : prefill_chunk_positions((block + 1) * tg);
-                const int at = single ? t - s_run - quotient(t - s_run, rule.tg_few, rule.few_magic) * rule.tg_few : same_seq ? p - block * tg : 0;
+                single = s_at + 1 + s_run.behind <= rule.short_tokens;
+                s_ct = single ? item_positions(rule, batch_own, p + s_run.behind + 1) : rule.tiles ? item_positions(rule, batch_own, (block + 1) * tg) : prefill_chunk_positions((block + 1) * tg);
+                const int at = single ? s_at : same_seq ? p - block * tg : 0;
                 if (at == 0) {                                                                     // rows of the sequence in this item, or in its aligned block
-                    s_tok = single ? min(rule.tg_few, behind + 1) : min(tg - (p - block * tg), 1 + ones_from(s_goes_on, WAVES + kAhead, tid + 1));
+                    s_tok = single ? 1 + s_run.behind : min(tg - (p - block * tg), 1 + s_run.behind);
                     s_n = (p + s_tok - 1 + s_ct) / s_ct;                                          // chunks the last of them reaches
                 }
             }
@@ -256,7 +248,9 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
             // block and chunk 20 us around its tiles
             const int p_subs = p_n ? r.keys >> 4 : 0, s_subs = s_n ? (p + s_tok + 15) >> 4 : 0;
             cost_items += 7 * ((few ? p_subs : 0) + (single ? s_subs : 0));
-            cost_blocks += (few ? 0 : p_subs * 8 + p_subs * 4 / rule.tg_many * p_tok + p_n * 320) + (single ? 0 : s_subs * 8 + s_subs * 4 / rule.tg_many * s_tok + s_n * 320);
+            auto block_cost = [&](int subs, int tok, int n) { return 8 * subs + quotient(4 * subs, rule.tg_many, rule.many_magic) * tok + n * 320; };
+            if (!few && p_n) cost_blocks += block_cost(p_subs, p_tok, p_n);
+            if (!single && s_n) cost_blocks += block_cost(s_subs, s_tok, s_n);
         }
         const int mine[3] = {(few ? p_n : 0) + (single ? s_n : 0), few ? 0 : p_n, single ? 0 : s_n};
         int start[3];
