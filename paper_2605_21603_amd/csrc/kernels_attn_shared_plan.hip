@@ -37,6 +37,7 @@ __device__ __forceinline__ int sum_all(int x) { return __builtin_amdgcn_readlane
 struct PlanRule {
     int tg_many, tg_few;                // tokens of a query block and of an item
     unsigned many_magic, few_magic;     // ceil(2^32 / .)
+    int ahead;                          // words of 64 rows that a query block takes
     int short_tokens;                   // a sequence of no more tokens than this in the step is served by items: a set of columns, which waves anywhere take
                                         // (64 of 2 to 8 tokens, 512 to 2048 keys of their own: 116 us with one alone, 112 so, 131 with up to two sets, which read their keys twice)
     int most_positions;                 // the longest chunk of an item's own keys
@@ -78,7 +79,7 @@ __device__ __forceinline__ bool by_items(const PlanRule &rule, long long batch, 
 // x / d by magic = ceil(2^32 / d), for d of at most 256 (0 for d = 1): exact below 2^24, and a division beyond.
 __device__ __forceinline__ int quotient(int x, int d, unsigned magic) { return magic && x < 1 << 24 ? (int)__umulhi((unsigned)x, magic) : x / d; }
 
-constexpr int kAhead = 4;                       // words behind a round: rows that go on with its last one's run or sequence
+constexpr int kAhead = 4;                       // words behind a round at most: rows that go on with its last one's run or sequence, as many as a query block has
 constexpr int kFewWaves = 4;
 // One workgroup, a thread per row and round of WAVES * 64 rows.  Four waves, one to a SIMD, where there are few rows: an instruction that sixteen go through
 // takes four times as long; those rows are one round, so nothing of them lies before or behind it.
@@ -173,11 +174,11 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         return Joined{at ? __builtin_amdgcn_readlane(x, at - 1) : empty, __builtin_amdgcn_readlane(x, 63)};
     };
     // The run that this thread's row lies in, of rows that each go on like the one before (a bit each; mine: this wave's): its first row, and how many of it are
-    // behind this row, up to kAhead words past the round.  before: the first row of the run that the round's last row lies in.
+    // behind this row, up to rule.ahead words past the round.  before: the first row of the run that the round's last row lies in.
     struct Run { int start, behind; };
     auto run_of = [&](const unsigned long long *words, unsigned long long mine, int t0, int &before) {
         const int at = __builtin_amdgcn_readfirstlane(wave);
-        const unsigned long long x = lane < (ONE ? WAVES : WAVES + kAhead) ? words[lane] : 0ull;
+        const unsigned long long x = lane < (ONE ? WAVES : WAVES + rule.ahead) ? words[lane] : 0ull;
         const int ones = x == ~0ull ? 64 : __ffsll(~x) - 1, last = 63 - __clzll((long long)~x);         // rows in front that go on, the last that does not
         const unsigned long long cut = __ballot(x != ~0ull), below = cut & ((1ull << at) - 1), all = cut & ((1ull << WAVES) - 1);
         const int next = __ffsll(cut >> (at + 1)) + at, beyond = (next - at - 1) * 64 + __builtin_amdgcn_readlane(ones, next);
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         const int shift = p - t;                                     // the same where positions follow one another, as items and query blocks take them to
         // rows behind this round that go on with its last one's run or sequence
         int ahead_seq = -1, ahead_pos = -1;
-        if (!ONE && tid < 64 * kAhead && t0 + ROUND + tid < rows) { ahead_seq = seq_of_token[t0 + ROUND + tid]; ahead_pos = pos_of_token[t0 + ROUND + tid]; }
+        if (!ONE && wave < rule.ahead && t0 + ROUND + tid < rows) { ahead_seq = seq_of_token[t0 + ROUND + tid]; ahead_pos = pos_of_token[t0 + ROUND + tid]; }
         next_seq = next_pos = -1;
         if (!ONE && t + ROUND < rows) { next_seq = seq_of_token[t + ROUND]; next_pos = pos_of_token[t + ROUND]; }
         if (lane == 63) { edge_lead[wave + 1] = on ? r.lead : -1; edge_keys[wave + 1] = r.keys; edge_seq[wave + 1] = s_seq; edge_shift[wave + 1] = shift; }
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         const bool same_prefix = on && lead_before == r.lead && keys_before == r.keys, same_seq = live && seq_before == s_seq && shift_before == shift;
         const unsigned long long p_mask = __ballot(same_prefix), s_mask = __ballot(same_seq);
         if (lane == 0) { p_goes_on[wave] = p_mask; s_goes_on[wave] = s_mask; }
-        if (!ONE && wave < kAhead) {
+        if (!ONE && wave < rule.ahead) {
             const Row x = row_of(ahead_seq, ahead_pos);
             const unsigned long long pm = __ballot(x.lead >= 0 && x.lead == edge_lead[WAVES] && x.keys == edge_keys[WAVES]);
             const unsigned long long sm = __ballot(x.pos >= 0 && x.seq * max_pages + x.pages == edge_seq[WAVES] && x.pos - x.keys - (t0 + ROUND + tid) == edge_shift[WAVES]);
@@ -356,7 +357,7 @@ hipError_t launch_attn_shared_plan(AttnForm form, const int32_t *seq_of_token, c
     if (p.n_seqs > kShareSeqs) p.lead = nullptr;
     const int many = form == SHARE_LISTS ? attn_prefill_block_tokens(sh) : 4 * TG;
     auto magic = [](int d) { return (unsigned)((0x100000000ull + d - 1) / d); };
-    const PlanRule rule{many, TG, magic(many), magic(TG), form == SHARE_LISTS ? TG : 1, sh.chunk_pages * sh.page_size, form == SHARE_TILES ? 128 : 64,
+    const PlanRule rule{many, TG, magic(many), magic(TG), (many + 63) / 64, form == SHARE_LISTS ? TG : 1, sh.chunk_pages * sh.page_size, form == SHARE_TILES ? 128 : 64,
                         form == SHARE_TILES || sh.page_size == 16 ? 128 : 64, sh.n_kv, form == SHARE_TILES};
     const bool small = std::max(rows, prefix.rows) <= kFewWaves * 64 && prefix.n_seqs <= 1024;       // (340 rows: 54 us in one round of 16 waves, 57 in two of 4)
     const auto kernel = form == SHARE_NOTHING ? attn_shared_plan_kernel<false, 16> : small ? attn_shared_plan_kernel<true, kFewWaves> : attn_shared_plan_kernel<true, 16>;
