@@ -307,13 +307,13 @@ __device__ __forceinline__ void attend_plain(const MendArgs &a, const bf16_t *q,
 // MEND: where the launch before found values that are not finite among those of later tokens than some column's, these met the column's zero probabilities
 // (0 * NaN), so all own keys are attended again, plainly, in that launch's chunks.
 template <typename T, bool BASE2, bool WIDE, bool SPLIT, bool MEND>
-__global__ __launch_bounds__(256) void attn_shared_combine_kernel(float *part_o, float *part_ml,
+__global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_combine_kernel(float *part_o, float *part_ml,
                                                                   const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
                                                                   const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct,
                                                                   int shared_slots, T *__restrict__ out, int ld_out, AttnShape sh,
                                                                   int32_t *__restrict__ counter0, int32_t *__restrict__ counter1, MendArgs mend) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    constexpr int SETS = WIDE ? 2 : 1, MOST_LOADS = 16 / SETS / (SPLIT ? 2 : 1), STEP = SPLIT ? 8 : 1;
+    constexpr int SETS = WIDE ? 2 : 1, MOST_LOADS = 8 / SETS, STEP = SPLIT ? 8 : 1;
     // the lists' query blocks have all been claimed: from the start again for the next layer
     if (counter0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) *(threadIdx.x ? counter1 : counter0) = 0;
     const int t = blockIdx.x, sub = threadIdx.x & 31, half = threadIdx.x >> 5, d = sh.head_dim, h = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * 8 + half;
@@ -377,7 +377,8 @@ __global__ __launch_bounds__(256) void attn_shared_combine_kernel(float *part_o,
                 }
             }
         };
-        // (rows of two to four chunks, prompts': 16 loads each, most of them the last chunk's again, took 24 us for 1563 rows of 32 heads, 4 take 19)
+        // (rows of two to four chunks, prompts': 16 loads each, most of them the last chunk's again, took 24 us for 1563 rows of 32 heads, 4 take 19; and with 8 for
+        // more chunks all registers of eight waves to a SIMD do: 5387 rows 75, 64 and so 45 us)
         if (!SPLIT && n <= 4) walk(std::integral_constant<int, 4>());
         else walk(std::integral_constant<int, MOST_LOADS>());
 #pragma unroll
