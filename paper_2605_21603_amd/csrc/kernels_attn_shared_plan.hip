@@ -48,14 +48,15 @@ struct PlanRule {
 
 // Chunks, from the batch, in sub-tiles of 16 positions: `shared` = keys of a prefix times query blocks that attend it, summed over the
 // prefixes; `own` = sequences' own keys, summed.  A chunk costs a partial set per column, written and read again, and too few of them
-// leave CUs idle.  Query blocks: what gives every CU (general form: one of four workgroups to a CU) a piece, or, beside items, what takes as long as those (a tile
+// leave CUs idle.  Query blocks: what gives three of four CUs (general form: one of four workgroups to a CU) a piece, so that
+// rounding leaves no second round of a few (256 tokens on 4 prefixes of 4096 to 8192, a piece for every CU: 77 us, so 64), or, beside items, what takes as long as those (a tile
 // of 64 positions some 2 us, keys of one kv head 512 bytes at 5 TB/s; in a third and a half of that, 64 tokens behind 2048 positions took 65 and 59 us and now take 60,
 // 256 behind 4 prefixes 275, 272 and 267, 64 of 4 drafts 97, 75 and 76, 256 of them 200, 192 and 187); two tiles at least, and at most 32 chunks a prefix.
 // All chunks of a prefix are then of one length, as a short last one would cost nearly all that a chunk does: as many as asked for (12 prompts of 33 to 300 tokens behind
 // 4096 keys: 202 -> 176 us), or, where query blocks have the chip to themselves, one fewer if that makes them at most half as long again (166 us; beside
 // items it delays the end, 256 tokens behind 4 prefixes 276 -> 295 us).
 __device__ __forceinline__ int block_positions(const PlanRule &rule, long long shared, long long own, int keys) {
-    const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 16, own * rule.n_kv * 3 / 64), ((long long)keys + 31) / 32);
+    const long long want = max(rule.tiles ? shared * rule.n_kv / 64 : max(shared * rule.n_kv / 12, own * rule.n_kv * 3 / 64), ((long long)keys + 31) / 32);
     const int ct = (int)min(max((want + 63) / 64 * 64, 128ll), 8192ll), n = max((keys + (shared > 8 * own && !rule.tiles ? ct / 2 : ct - 1)) / ct, (keys + 8191) / 8192);
     return ((keys + n - 1) / n + 63) / 64 * 64;
 }
