@@ -7,9 +7,9 @@
 // them an attention of every sequence for itself, as a decode's or a prompt's that starts at P.  Three launches: the plan
 // (kernels_attn_shared_plan.hip), the keys (attn_shared_kernel, or attn_tile of kernels_attn_generic.hip for what it does not
 // take), and the merge of a row's chunks.
-// 32 q heads, 8 kv heads, 128 wide, caches out of reach of the last call, plan + keys + merge: 5 tokens behind 512 positions 5.6 + 6.7 + 4.4 us; 64 behind 2048 with
-// 16 to 1024 of their own, 162 MB, 6.1 + 49 + 5.4; 256 on 4 prefixes, 1.19 GB, 7.6 + 253 (4.7 TB/s) + 9.9; 12 prompts of 33 to 300 tokens behind 4096 positions, 1.08e11
-// operations, 15.8 + 158 (0.68 PFLOP/s) + 25.
+// 32 q heads, 8 kv heads, 128 wide, caches out of reach of the last call, plan + keys + merge: 5 tokens behind 512 positions 5.4 + 6.8 + 4.2 us; 64 behind 2048 with
+// 16 to 1024 of their own, 162 MB, 6.0 + 49 + 5.4; 256 on 4 prefixes, 1.19 GB, 6.8 + 250 (4.7 TB/s) + 9.6; 12 prompts of 33 to 300 tokens behind 4096 positions, 1.08e11
+// operations, 13 + 150 (0.72 PFLOP/s) + 14.
 #include <algorithm>
 #include <atomic>
 
