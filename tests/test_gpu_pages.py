@@ -223,3 +223,32 @@ def test_two_streams_and_two_pools():
         c.model.fork([0, 1], [4, 5])
     a.check()
     b.check()
+
+
+def test_pools_beyond_32_bit_offsets():
+    """Pages whose bytes lie beyond 2^32 are copied, forked from and moved to the front."""
+    n, ps = 140000, 16
+    k, v = (torch.zeros((1, n, 8, a, b), dtype=torch.bfloat16, device=DEV) for a, b in ((ps, 128), (128, ps)))
+    ints = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    last = list(range(n - 5, n))
+    k[0, n - 5:], v[0, n - 5:] = torch.randn((5, 8, ps, 128), device=DEV).bfloat16(), torch.randn((5, 8, 128, ps), device=DEV).bfloat16()
+    want_k, want_v = k[0, n - 5:].clone(), v[0, n - 5:].clone()
+    table, lens, ref = torch.zeros((3, 6), dtype=torch.int32, device=DEV), ints([5 * ps - 3, 0, 0]), torch.zeros(n, dtype=torch.int32, device=DEV)
+    table[0, :5] = ints(last)
+    ref[n - 5:] = 1
+    ref[:n - 5] = 1                                                   # nothing is free below
+    ref[n - 7:n - 5] = 0
+    pool = B.PagePool(k, v, table, lens, ref, 2)
+    assert pool.fork(ints([0, 0]), ints([1, 2])).tolist() == [B.DYN_PAGES_DONE] * 2
+    assert table[1, :5].tolist() == last[:4] + [n - 7] and table[2, :5].tolist() == last[:4] + [n - 6]
+    for p in (n - 7, n - 6):
+        assert torch.equal(k[0, p], want_k[4]) and torch.equal(v[0, p], want_v[4])
+    pool.copy(ints([n - 3, n - 1]), ints([7, n - 2]))
+    assert torch.equal(k[0, 7], want_k[2]) and torch.equal(v[0, 7], want_v[2]) and torch.equal(k[0, n - 2], want_k[4])
+    ref[:n - 7] = 0                                                   # all but the rows' pages are free
+    want = [(k[0, p].clone(), v[0, p].clone()) for p in range(n - 7, n)]
+    new_page, n_live = pool.compact()
+    assert n_live.tolist() == [7] and new_page[n - 7:].tolist() == list(range(7)) and (new_page[:n - 7] == -1).all()
+    for p, (a, b) in enumerate(want):
+        assert torch.equal(k[0, p], a) and torch.equal(v[0, p], b)
+    assert table[1, :5].tolist() == [2, 3, 4, 5, 0] and ref[:7].tolist() == [1, 1, 3, 3, 3, 3, 1] and not ref[7:].any()
