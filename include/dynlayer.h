@@ -469,7 +469,8 @@ dyn_status dyn_tune(dyn_layer *layer, const dyn_batch *batch, const int32_t *ctx
  *
  * Causal paged attention of n_tokens query rows, outside a layer: row t is a token of sequence seq_of_token[t] at position
  * pos_of_token[t] and attends the cached keys 0 .. pos of that sequence (all of them are in the cache: nothing is appended, nothing
- * rotated), scaled by 1 / sqrt(head_dim).  A row of position -1 attends nothing and its output is zero.
+ * rotated), scaled by 1 / sqrt(head_dim).  A row of position -1, or whose sequence or position lies outside the block table,
+ * attends nothing and its output is zero.  The table's entries up to every row's position are pages of the pools.
  * prefix_lead[s] and prefix_pages[s] say what sequences have in common: the first prefix_pages[s] pages of row s of the block
  * table are those of row prefix_lead[s], and every sequence with that lead and that many pages shares them (a sequence
  * that shares nothing: 0 pages).  Shared pages are read once, through the lead's row, for all rows of adjacent tokens whose sequences

@@ -98,6 +98,8 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
     __shared__ int sums[3][WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ps = sh.page_size, max_pages = sh.max_pages_per_seq;
     const bool any = SHARE && prefix.lead != nullptr;
+    // a row whose sequence or position lies outside the table attends nothing, as one of position -1
+    auto inside = [&](int seq, int pos) { return (unsigned)seq < (unsigned)prefix.n_seqs && pos < max_pages * ps ? pos : -1; };
     int next_seq = -1, next_pos = -1;                                // the next round's row, on its way
     if (tid < rows) { next_seq = seq_of_token[tid]; next_pos = pos_of_token[tid]; }
     if (tid < 2) batch[tid] = cost[tid] = 0;
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         int shared = 0, own = 0;
         for (int t = tid; t < prefix.rows; t += ROUND) {
             const int seq = prefix.seq_of_token[t], before = prefix.seq_of_token[max(t - 1, 0)];
-            const Row r = row_of(seq, prefix.pos_of_token[t]);
+            const Row r = row_of(seq, inside(seq, prefix.pos_of_token[t]));
             if (r.lead >= 0) {
                 atomicAdd(&members[r.lead], 1);
                 shared += r.keys >> 4;
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
     int cost_items = 0, cost_blocks = 0;
     for (int t0 = 0; t0 < rows; t0 += ROUND) {
         const int t = t0 + tid;
-        const Row r = row_of(next_seq, next_pos);
+        const Row r = row_of(next_seq, inside(next_seq, next_pos));
         const bool on = r.lead >= 0, live = t < rows;
         const int s_seq = !live ? -2 : r.pos < 0 ? -3 - t : r.seq * max_pages + r.pages, p = r.pos - r.keys;
         const int shift = p - t;                                     // the same where positions follow one another, as items and query blocks take them to
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
         const unsigned long long p_mask = __ballot(same_prefix), s_mask = __ballot(same_seq);
         if (lane == 0) { p_goes_on[wave] = p_mask; s_goes_on[wave] = s_mask; }
         if (!ONE && wave < rule.ahead) {
-            const Row x = row_of(ahead_seq, ahead_pos);
+            const Row x = row_of(ahead_seq, inside(ahead_seq, ahead_pos));
             const unsigned long long pm = __ballot(x.lead >= 0 && x.lead == edge_lead[WAVES] && x.keys == edge_keys[WAVES]);
             const unsigned long long sm = __ballot(x.pos >= 0 && x.seq * max_pages + x.pages == edge_seq[WAVES] && x.pos - x.keys - (t0 + ROUND + tid) == edge_shift[WAVES]);
             if (lane == 0) { p_goes_on[WAVES + wave] = pm; s_goes_on[WAVES + wave] = sm; }

@@ -318,6 +318,16 @@ def test_rows_around_the_plans_rounds(rows):
     c.check(got)
 
 
+@pytest.mark.parametrize("shape", ["fast", "fast_p48", "bf16_64", "f32_32", "odd_page"])
+def test_rows_outside_the_table_attend_nothing(shape):
+    """Sequences that are none and positions past the table's width, between rows that are read as ever."""
+    c = Case(shape, group("a", 3, [5, 40, 7]) + group("a", 3, [30, 20], new=9) + [(None, 0, 50, 20), ("a", 3, 4, 1)])
+    n, most = len(c.ctx), c.table.shape[1] * SHAPES[shape][3]
+    for t, (seq, pos) in {1: (n, 3), 4: (-1, 0), 8: (0, most), 15: (2 ** 31 - 1, 9), 16: (1, 2 ** 31 - 1), 25: (-2 ** 31, 5), 40: (n, most), 41: (3, -7)}.items():
+        c.args["seq_of_token"][t], c.args["pos_of_token"][t], c.pos[t] = seq, pos, -1
+    c.check(c.run())
+
+
 @pytest.mark.parametrize("n_seqs", [1024, 1025])
 def test_few_rows_of_many_sequences(n_seqs):
     """The plan of few rows counts up to 1024 sequences' leads; a batch may have many more sequences than rows."""
