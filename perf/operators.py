@@ -406,7 +406,7 @@ def _plain_fork(s, parent, child):
     entry = has_tail[:, None] & (cols == full[:, None])
     table[child] = torch.where(shared, rows, torch.where(entry, fresh[:, None], table[child]))
     s["seq_len"][child] = torch.where(ok, lens, 0)
-    _plain_copy(s, last, torch.where(has_tail, fresh, last))
+    _plain_copy(s, last[has_tail], fresh[has_tail])
     return torch.where(ok, 0, 1).to(torch.int32)
 
 
@@ -430,7 +430,7 @@ def _plain_resize(s, row, length):
     _add_refs(s, fresh, split, 1)
     table[row] = torch.where(grown, taken, torch.where(entry, fresh[:, None], rows))
     s["seq_len"][row] = torch.where(ok, length, before)
-    _plain_copy(s, last, torch.where(split, fresh, last))
+    _plain_copy(s, last[split], fresh[split])
     return torch.where(ok, 0, 1).to(torch.int32)
 
 
