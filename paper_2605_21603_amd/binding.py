@@ -562,9 +562,45 @@ class DeviceStep:
         torch.cuda.synchronize(dev)
 
 
-def _stream_of(stream: Optional[torch.cuda.Stream], device) -> C.c_void_p:
-    # (the raw handle: building torch's Stream object takes 2 us, as long as a small call's kernel)
-    return C.c_void_p(stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index))
+class _Workspace:
+    """A handle's device bytes, used by its calls on whatever streams they are made.  Torch gives a block back to the stream it was taken on: other
+    streams wait for what was queued there before, once, and the block is kept until their work is done when the handle is dropped."""
+
+    def __init__(self, given: Optional[torch.Tensor], nbytes: int, device):
+        self.device = device
+        self.bytes = given if given is not None else torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self._known = {torch._C._cuda_getCurrentRawStream(device.index)}
+        with torch.cuda.device(device):
+            self._made = None if torch.cuda.is_current_stream_capturing() else torch.cuda.current_stream().record_event()
+
+    def aligned(self) -> int:
+        return (self.bytes.data_ptr() + 255) & ~255
+
+    def stream(self, stream: Optional[torch.cuda.Stream], *arrays: torch.Tensor) -> C.c_void_p:
+        """The raw handle of a call's stream, by default torch's current one.  A stream of the call's own is through with its `arrays` before their
+        memory is another tensor's."""
+        # (building torch's Stream object takes 2 us, as long as a small call's kernel)
+        raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(self.device.index)
+        if raw not in self._known:
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+                on = torch.cuda.current_stream()
+                self.bytes.record_stream(on)
+                if not torch.cuda.is_current_stream_capturing():       # (a capture comes after all that was queued)
+                    if self._made is not None:
+                        on.wait_event(self._made)
+                    self._known.add(raw)
+        if stream is not None:
+            for t in arrays:
+                t.record_stream(stream)
+        return C.c_void_p(raw)
+
+
+def _empty_on(stream: Optional[torch.cuda.Stream], n: int, device) -> torch.Tensor:
+    """An int32 result that a kernel on `stream` writes: its memory is that stream's, which no other tensor has before or behind it in another order."""
+    if stream is None:
+        return torch.empty(n, dtype=torch.int32, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.int32, device=device)
 
 
 _current_device = torch._C._cuda_getDevice
@@ -630,16 +666,17 @@ class SharedAttention:
             raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error())
         if workspace is not None and (workspace.dtype != torch.uint8 or workspace.device != self.device or workspace.numel() < nbytes + 256):
             raise ValueError("workspace: %d bytes on %s" % (nbytes + 256, self.device))
-        self.workspace = workspace if workspace is not None else torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
-        self.batch.workspace = (self.workspace.data_ptr() + 255) & ~255
+        self._workspace = _Workspace(workspace, nbytes + 256, self.device)
+        self.workspace = self._workspace.bytes
+        self.batch.workspace = self._workspace.aligned()
         self.batch.workspace_bytes = nbytes
 
     def forward(self, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
-        """Writes and returns `out`; on `stream`, by default torch's current one."""
+        """Writes and returns `out`; on `stream`, by default torch's current one, which has to come after what made the tensors."""
         if _current_device() != self.device.index:                    # a launch on another device's stream is an error
             with torch.cuda.device(self.device):
                 return self.forward(stream)
-        _check(lib().dyn_attn_shared(C.byref(self.batch), _stream_of(stream, self.device)))
+        _check(lib().dyn_attn_shared(C.byref(self.batch), self._workspace.stream(stream)))
         return self.out
 
 
@@ -648,8 +685,8 @@ class PagePool:
 
     k_cache [layers, pages, kv heads, page size, head dim] and v_cache [layers, pages, kv heads, head dim, page size], or lists of
     one tensor per layer; block_table [rows, pages per row], seq_len [rows] and ref_count [pages] int32, all on one device.
-    The calls run on `stream` (default: torch's current one on that device), change the tensors in place and wait for
-    nothing.  max_requests: the most requests a fork or resize will have; the workspace is sized for it."""
+    The calls run on `stream` (default: torch's current one on that device; it has to come after what made the tensors), change the tensors in
+    place and wait for nothing; results that a call makes are that stream's.  max_requests: the most requests a fork or resize will have; the workspace is sized for it."""
 
     def __init__(self, k_cache, v_cache, block_table: torch.Tensor, seq_len: torch.Tensor, ref_count: torch.Tensor, max_requests: int):
         ks, vs = list(k_cache), list(v_cache)
@@ -670,8 +707,8 @@ class PagePool:
         nbytes = lib().dyn_pages_workspace_bytes(C.byref(self.pool), self.max_requests)
         if nbytes == 0:
             raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error() or "max_requests = %d" % self.max_requests)
-        self._workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
-        self.pool.workspace = (self._workspace.data_ptr() + 255) & ~255
+        self._workspace = _Workspace(None, nbytes + 256, self.device)
+        self.pool.workspace = self._workspace.aligned()
         self.pool.workspace_bytes = nbytes
 
     def copy(self, src: torch.Tensor, dst: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
@@ -681,7 +718,7 @@ class PagePool:
                 return self.copy(src, dst, stream)
         n = len(src)
         _check(lib().dyn_pages_copy(C.byref(self.pool), n, _int32(src, "src", self.device, (n,)), _int32(dst, "dst", self.device, (n,)),
-                                    _stream_of(stream, self.device)))
+                                    self._workspace.stream(stream, src, dst)))
 
     def _requests(self, call, a, b, names, status, stream) -> torch.Tensor:
         if _current_device() != self.device.index:
@@ -689,9 +726,9 @@ class PagePool:
                 return self._requests(call, a, b, names, status, stream)
         n = len(a)
         if status is None:
-            status = torch.empty(n, dtype=torch.int32, device=self.device)
+            status = _empty_on(stream, n, self.device)
         _check(call(C.byref(self.pool), n, _int32(a, names[0], self.device, (n,)), _int32(b, names[1], self.device, (n,)),
-                    _int32(status, "status", self.device, (n,)), _stream_of(stream, self.device)))
+                    _int32(status, "status", self.device, (n,)), self._workspace.stream(stream, a, b, status)))
         return status
 
     def fork(self, parent: torch.Tensor, child: torch.Tensor, status: Optional[torch.Tensor] = None,
@@ -710,8 +747,8 @@ class PagePool:
             with torch.cuda.device(self.device):
                 return self.compact(new_page, n_live, stream)
         n = self.pool.n_pages
-        new_page = torch.empty(n, dtype=torch.int32, device=self.device) if new_page is None else new_page
-        n_live = torch.empty(1, dtype=torch.int32, device=self.device) if n_live is None else n_live
+        new_page = _empty_on(stream, n, self.device) if new_page is None else new_page
+        n_live = _empty_on(stream, 1, self.device) if n_live is None else n_live
         _check(lib().dyn_pages_compact(C.byref(self.pool), _int32(new_page, "new_page", self.device, (n,)), _int32(n_live, "n_live", self.device, (1,)),
-                                       _stream_of(stream, self.device)))
+                                       self._workspace.stream(stream, new_page, n_live)))
         return new_page, n_live
