@@ -84,7 +84,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                                                               float *__restrict__ part_o, float *__restrict__ part_ml,
                                                               AttnShape sh, const int32_t *__restrict__ plan, int32_t *__restrict__ counter,
                                                               const int32_t *__restrict__ ct_of_token, int ld_q = 0, SubTiles page = SubTiles{},
-                                                              int32_t *odd = nullptr) {
+                                                              int32_t *odd = nullptr, int mark = 0) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int32_t *pid = reinterpret_cast<int32_t *>(lds + kRing * kTile);      // physical pages of the chunk
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -145,7 +145,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
         // keys its first token attends; columns of dead tokens or heads carry zeros and are never stored
         const int wave_min_keys = wave_tok0 < n_tok ? pos_of_token[t0 + wave_tok0] + 1 : 0;
         __syncthreads();                                                  // pid is visible
-        // PARTS: values behind the block's first token, which some columns must not see: *odd is set if they are not all finite
+        // PARTS: values behind the block's first token, which some columns must not see: its rows are marked in `odd` if they are not all finite
         if constexpr (PARTS) {
             const int late0 = max(pos_of_token[t0] + 1, lp0 * PS), late1 = min(n_keys, (lp0 + n_pg) * PS), per = WIDE_PAGES ? page.per : 1;
             const int most = late0 < late1 ? ((late1 + PS - 1) / PS - late0 / PS) * 256 : 0;
@@ -160,7 +160,10 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                     found |= at >= late0 && at < late1 && (x[d] & 0x7f80u) == 0x7f80u;
                     found |= at + 1 >= late0 && at + 1 < late1 && (x[d] & 0x7f800000u) == 0x7f800000u;
                 }
-                if (found) *odd = 1;
+                if (found) {
+#pragma clang loop unroll(disable)
+                    for (int j = 0; j < n_tok; ++j) odd[t0 + j] = mark;
+                }
             }
         }
 

@@ -81,7 +81,7 @@ dyn_status dyn_attn_shared(const dyn_attn_batch *b, void *hip_stream) {
     char *const base = (char *)b->workspace;
     const hipError_t e = dyn::launch_attention_shared(b->dtype, b->q, b->ld_q, b->seq_of_token, b->pos_of_token, b->block_table, b->k_cache, b->v_cache, b->out, b->ld_out,
                                                       (float *)(base + w.part_o), (float *)(base + w.part_ml), (int32_t *)(base + w.plan), sh, prefix,
-                                                      b->n_tokens, (hipStream_t)hip_stream, nullptr, nullptr, false);
+                                                      b->n_tokens, (hipStream_t)hip_stream, nullptr, nullptr, 0);
     if (e != hipSuccess) return fail(DYN_ERR_HIP, "launch of the attention failed: %s", hipGetErrorString(e));
     return DYN_OK;
 }

@@ -28,6 +28,7 @@ struct SharedArgs {
     const int32_t *block_table;
     SharedPlan plan;
     AttnShape sh;                         // rows of a table of one wide row; max_chunks: of both halves
+    int mark;                             // what this launch writes into plan.odd
     int ld_q, shared_slots;               // partials of own keys lie behind shared_slots chunks of shared ones
     float *part_o, *part_ml;
     prefill::SubTiles page;
@@ -151,7 +152,10 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
                     for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) found |= late_odd(vr[B][i][dt][h], at + 16 * i + 4 * lq + 2 * h, m.full);
-                    if (found) *a.plan.odd = 1;
+                    if (found) {
+#pragma clang loop unroll(disable)
+                        for (int j = 0; j < m.n_tok; ++j) a.plan.odd[m.t + j] = a.mark;
+                    }
                 }
             }
         }
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(Sh
         int32_t *const list = own ? w.s_blocks : w.p_blocks;
         if (list[0] == 0) continue;
         prefill::attn_prefill_items<true, WIDE_PAGES>(a.q, own ? w.s_seq : w.p_seq, own ? w.s_pos : w.p_pos, a.block_table, a.k, a.v, nullptr, 0,
-                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q, a.page, w.odd);
+                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q, a.page, w.odd, a.mark);
     }
 }
 
@@ -257,7 +261,7 @@ __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(Sh
 struct MendArgs {
     const bf16_t *q, *k, *v;
     const int32_t *block_table, *s_seq, *odd;
-    int ld_q;
+    int mark, ld_q;
 };
 
 // Positions first .. end - 1 for one column (q: its 128 values), by a half-wave: a position to a lane for the scores, four head-dim indices for the values, and
@@ -304,8 +308,9 @@ __device__ __forceinline__ void attend_plain(const MendArgs &a, const bf16_t *q,
 // 128).  Where there are rows to fill the chip a half-wave merges a (token, q head); else (SPLIT) a workgroup does, its eight half-waves every
 // eighth chunk each and the eight results in order through LDS.  A row without keys is zero.  What it costs is two dependent loads, of the row's chunk counts and
 // of its partials, so the first of those are all on their way beside the maxima and sums that weigh them.
-// MEND: where the launch before found values that are not finite among those of later tokens than some column's, these met the column's zero probabilities
-// (0 * NaN), so all own keys are attended again, plainly, in that launch's chunks.
+// MEND: where the launch before found values that are not finite among those of later tokens than a row's, in what the row was served with, these met its
+// zero probabilities (0 * NaN), so all its own keys are attended again, plainly, in that launch's chunks.  Sequences are whole in a dispatch, so which rows
+// these are does not depend on the schedule.
 template <typename T, bool BASE2, bool WIDE, bool SPLIT, bool MEND>
 __global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_combine_kernel(float *part_o, float *part_ml,
                                                                   const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
@@ -318,7 +323,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_com
     if (counter0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) *(threadIdx.x ? counter1 : counter0) = 0;
     const int t = blockIdx.x, sub = threadIdx.x & 31, half = threadIdx.x >> 5, d = sh.head_dim, h = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * 8 + half;
     if (h >= sh.n_q) return;
-    const int pp = p_pos[t], sp = s_pos[t], pc = p_ct[t], sc = s_ct[t];
+    const int pp = p_pos[t], sp = s_pos[t], pc = p_ct[t], sc = s_ct[t], odd = MEND ? mend.odd[t] : 0;
     const int n_shared = pp < 0 ? 0 : (pp + pc) / pc, n = n_shared + (sp < 0 ? 0 : (sp + sc) / sc);
     const int c0 = SPLIT ? half : 0, count = (n - c0 + STEP - 1) / STEP;                     // chunks c0, c0 + STEP, ...
     f32x4 acc[SETS];
@@ -333,7 +338,7 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_com
             return first + (size_t)(c < n_shared ? c : shared_slots + c - n_shared) * next;
         };
         if constexpr (MEND) {
-            if (*mend.odd) {
+            if (odd == mend.mark) {
 #pragma clang loop unroll(disable)
                 for (int i = 0; i < count; ++i) {
                     const int c = c0 + i * STEP - n_shared, g = h / (sh.n_q / sh.n_kv);
@@ -430,12 +435,12 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_com
 
 hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int32_t *seq_of_token, const int32_t *pos_of_token, const int32_t *block_table,
                                    const void *k_cache, const void *v_cache, void *out, int ld_out, float *part_o, float *part_ml, int32_t *plan,
-                                   const AttnShape &sh, const AttnPrefix &prefix, int rows, hipStream_t s, hipEvent_t mid, hipEvent_t pre, bool plan_ready) {
+                                   const AttnShape &sh, const AttnPrefix &prefix, int rows, hipStream_t s, hipEvent_t mid, hipEvent_t pre, int layer) {
     if (rows <= 0) return hipSuccess;
     if (rows >= 1 << 24) return hipErrorInvalidConfiguration;
     const AttnForm form = attn_shared_form(dtype, sh, k_cache, v_cache);
     const SharedPlan w = attn_shared_plan(plan, sh, prefix, rows);
-    hipError_t e = plan_ready ? hipSuccess : launch_attn_shared_plan(form, seq_of_token, pos_of_token, sh, prefix, rows, w, s);
+    hipError_t e = layer > 0 ? hipSuccess : launch_attn_shared_plan(form, seq_of_token, pos_of_token, sh, prefix, rows, w, s);
     if (e == hipSuccess && pre) e = hipEventRecord(pre, s);
     if (e != hipSuccess) return e;
     AttnShape part = sh;
@@ -452,7 +457,7 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
             if (e != hipSuccess) return e;
             attr_set[sh.page_size != 16] |= bit;
         }
-        const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, ld_q, prefix.max_chunks, part_o,
+        const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, layer + 1, ld_q, prefix.max_chunks, part_o,
                            part_ml, prefill::SubTiles{sh.page_size / 16, (unsigned)((0x100000000ull + sh.page_size / 16 - 1) / (sh.page_size / 16))}};
         const long most = (long)rows * sh.n_kv * part.max_chunks;
         const int cus = sh.n_cus > 0 && sh.n_cus < 256 ? sh.n_cus : 256;
@@ -470,7 +475,7 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
     // which of the two depends on the batch, so that a row's bits do not depend on the dispatch it is in
     const bool split = (long)prefix.rows * sh.n_q <= 512;
     const dim3 grid(rows, split ? sh.n_q : (sh.n_q + 7) / 8), block(256);
-    const MendArgs mend{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w.s_seq, w.odd, ld_q};
+    const MendArgs mend{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w.s_seq, w.odd, layer + 1, ld_q};
 #define DYN_COMBINE_AS(T, B2, WIDE, SPLIT, MEND)                                                                                                            \
     hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE, SPLIT, MEND>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,        \
                        prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, lists ? w.s_blocks + 1 : nullptr, mend)
