@@ -73,6 +73,21 @@ struct SubTiles {
     __device__ __forceinline__ int page_of(int sub) const { return (int)__umulhi((unsigned)sub, magic); }     // exact for sub * per below 2^32
 };
 
+// bf16 numbers that a probability is the sum of in its product with V.  Pages of 16: one, rounded as in the layer's own kernels for these shapes (2^-8 of it).  Larger
+// pages without shared prefixes run in the general form with all 24 bits, so with them a probability is two, to 2^-16 of it: the outputs' error against 64 bits is
+// the general form's to three digits (0.00166 of their norm; one part 0.0023, three 0.00166).  32 q heads, 8 kv heads, pages of 32, one / two / three parts / general form:
+// 256 tokens on 4 prefixes 289 / 289 / 298 / 453 us, 64 of 2 to 5 tokens 85 / 97 / 109 / 111, 12 prompts behind 4096 positions 173 / 211 / 253 / 849.
+constexpr int parts_of_p(bool wide_pages) { return wide_pages ? 2 : 1; }
+// Four fp32 numbers as the sums of N bf16 numbers each.
+template <int N>
+__device__ __forceinline__ void bf16_parts(f32x4 p, u32x2 (&w)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        w[k] = __builtin_bit_cast(u32x2, __builtin_convertvector(p, bf16x4));
+        if (k + 1 < N) p -= f32x4{__uint_as_float(w[k][0] << 16), __uint_as_float(w[k][0] & 0xffff0000u), __uint_as_float(w[k][1] << 16), __uint_as_float(w[k][1] & 0xffff0000u)};
+    }
+}
+
 template <bool PARTS = false, bool WIDE_PAGES = false>
 __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qkv,
                                                               const int32_t *__restrict__ seq_of_token,
@@ -241,7 +256,8 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
         // tile i - 1 and the V slot of tile i - 2 are free: the early waves issue K of tile i + 2, the late ones V of
         // tile i + 1, and what phase 2 i reads has landed when each wave's loads but the last four have.
         f32x4 sv[kSets][kTP];                                             // raw scores q . k of the tile in flight
-        bf16x8 pb[kSets][kTP / 2];                                        // probabilities: one k = 32 operand per pair of pages
+        constexpr int NP = parts_of_p(WIDE_PAGES);
+        bf16x8 pb[NP][kSets][kTP / 2];                                    // probabilities, in NP bf16 parts: one k = 32 operand per pair of pages
         auto visible = [&](int ti) { return (lp0 + kTP * ti) * PS < wave_keys; };   // wave-uniform: some position of the tile is
         // the query operands are in their registers before the first direct load is issued: a wait for them
         // inside the loop would be a wait for the ring
@@ -278,12 +294,14 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                     });
                 };
                 read_v(vx[0], std::integral_constant<int, 0>());
-                // the denominator sums the probabilities exactly as the value product sees them (rounded
-                // to bf16): one more matrix product, against a block of ones
+                // the denominator sums the probabilities exactly as the value product sees them (in
+                // bf16 parts): one more matrix product each, against a block of ones
 #pragma unroll
-                for (int pp = 0; pp < kTP / 2; ++pp)
+                for (int k = NP - 1; k >= 0; --k)
 #pragma unroll
-                    for (int q = 0; q < kSets; ++q) acc_l[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[q][pp], acc_l[q], 0, 0, 0);
+                    for (int pp = 0; pp < kTP / 2; ++pp)
+#pragma unroll
+                        for (int q = 0; q < kSets; ++q) acc_l[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[k][q][pp], acc_l[q], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 static_for<0, 8>([&](auto dt_c) {
                     constexpr int dt = decltype(dt_c)::value;
@@ -299,8 +317,10 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                         const u32x2 x0 = vx[dt & 1][2 * pp], x1 = vx[dt & 1][2 * pp + 1];
                         const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{x0[0], x0[1], x1[0], x1[1]});
 #pragma unroll
-                        for (int q = 0; q < kSets; ++q)
-                            acc[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[q][pp], acc[q][dt], 0, 0, 0);
+                        for (int k = NP - 1; k >= 0; --k)
+#pragma unroll
+                            for (int q = 0; q < kSets; ++q)
+                                acc[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[k][q][pp], acc[q][dt], 0, 0, 0);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 });
@@ -387,9 +407,11 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                             p0[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[q][2 * pp][r], sscale, -m_ref));
                             p1[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[q][2 * pp + 1][r], sscale, -m_ref));
                         }
-                        const u32x2 w0 = __builtin_bit_cast(u32x2, __builtin_convertvector(p0, bf16x4));
-                        const u32x2 w1 = __builtin_bit_cast(u32x2, __builtin_convertvector(p1, bf16x4));
-                        pb[q][pp] = __builtin_bit_cast(bf16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
+                        u32x2 w0[NP], w1[NP];
+                        bf16_parts<NP>(p0, w0);
+                        bf16_parts<NP>(p1, w1);
+#pragma unroll
+                        for (int k = 0; k < NP; ++k) pb[k][q][pp] = __builtin_bit_cast(bf16x8, u32x4{w0[k][0], w0[k][1], w1[k][0], w1[k][1]});
                     }
                 }
                 if (__any(rescale)) {

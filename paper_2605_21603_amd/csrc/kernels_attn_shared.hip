@@ -72,7 +72,7 @@ __device__ __forceinline__ Item fetch_item(const SharedArgs &a, int i) {
 // to every wave: of the two waves of a SIMD the older gets its loads first, and with equal shares - 256 tokens of 1024 keys - the older ones were through
 // after 149 us and the others after 196.)  K and V go from memory straight into MFMA operand layout,
 //     S[16 pos, 16 cols]  = K_sub[16, 128] Q^T[128, 16]       (4 x mfma 16x16x32 per sub-tile)
-//     O^T[128, 16 cols]  += V^T[128, 32] P[32, 16]            (8 x mfma 16x16x32 per pair of sub-tiles)
+//     O^T[128, 16 cols]  += V^T[128, 32] P[32, 16]            (8 x mfma 16x16x32 per pair of sub-tiles and part of P)
 // with the D layout of the first product (lane: column l % 16, positions 4 (l / 16) + r) the B layout of the second.  Two register
 // buffers of 32 positions; the last pair of a chunk is followed by the first of the wave's next item, whose indices were
 // fetched while this one was multiplied.
@@ -168,23 +168,29 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
         l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) acc[dt] *= alpha;
-        // probabilities are rounded to bf16 for the matrix product, and the same rounded ones are summed
-        u32x2 w[TILE];
+        // probabilities go into the matrix product in NP bf16 parts (parts_of_p), and what goes in is what is summed
+        constexpr int NP = prefill::parts_of_p(WIDE_PAGES);
+        u32x2 w[TILE][NP];
 #pragma unroll
         for (int i = 0; i < TILE; ++i) {
             f32x4 p;
 #pragma unroll
             for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(s[i][r] - ref);
-            w[i] = __builtin_bit_cast(u32x2, __builtin_convertvector(p, prefill::bf16x4));
-            l_run += (__uint_as_float(w[i][0] << 16) + __uint_as_float(w[i][0] & 0xffff0000u)) + (__uint_as_float(w[i][1] << 16) + __uint_as_float(w[i][1] & 0xffff0000u));
+            prefill::bf16_parts<NP>(p, w[i]);
+#pragma unroll
+            for (int k = NP - 1; k >= 0; --k)
+                l_run += (__uint_as_float(w[i][k][0] << 16) + __uint_as_float(w[i][k][0] & 0xffff0000u)) + (__uint_as_float(w[i][k][1] << 16) + __uint_as_float(w[i][k][1] & 0xffff0000u));
         }
 #pragma unroll
         for (int i = 0; i < TILE; i += 2) {
-            const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{w[i][0], w[i][1], w[i + 1][0], w[i + 1][1]});
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) {
-                const u32x2 x = vr[B][i][dt], y = vr[B][i + 1][dt];
-                acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}), pb, acc[dt], 0, 0, 0);
+            for (int k = NP - 1; k >= 0; --k) {
+                const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{w[i][k][0], w[i][k][1], w[i + 1][k][0], w[i + 1][k][1]});
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    const u32x2 x = vr[B][i][dt], y = vr[B][i + 1][dt];
+                    acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]}), pb, acc[dt], 0, 0, 0);
+                }
             }
         }
     };
