@@ -92,6 +92,12 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
     static_assert(WAVES >= kAhead, "a wave per word of rows ahead");
     // per sequence: its lead (-1: none), pages, whether items serve its shared keys (the sign) and their chunks; per lead: who shares
     __shared__ int lead_of[SHARE ? kShareSeqs : 1], pages_of[SHARE ? kShareSeqs : 1], rule_of[SHARE && WAVES != kFewWaves ? kShareSeqs : 1], members[SHARE ? kShareSeqs : 1];
+    // per sequence, where there are enough rows for a long prompt (prompt_chunk_positions, whose rule it is): its rows of the batch, and the first one's own
+    // position.  Its blocks of own keys have longer chunks: 4096 tokens alone 259 -> 230 us, behind 2000 positions of their own 425 -> 380, 6000 751 -> 598, 4096
+    // beside 64 decodes 402 -> 370; 5387 rows of 242 sequences 202 -> 203.5.
+    constexpr bool RUNS = SHARE && WAVES != kFewWaves;
+    __shared__ int run_start[RUNS ? kShareSeqs : 1], run_end[RUNS ? kShareSeqs : 1], run_pos[RUNS ? kShareSeqs : 1];
+    const bool long_prompts = RUNS && !rule.tiles && prefix.rows > kLongRun && prefix.n_seqs <= kShareSeqs;
     __shared__ int batch[2], cost[2];                                // sub-tiles of shared and of own keys; what the lists take, in 1/16 us
     __shared__ int edge_lead[WAVES + 1], edge_keys[WAVES + 1], edge_seq[WAVES + 1], edge_shift[WAVES + 1];       // the last row of each wave's 64, and of the round before
     __shared__ unsigned long long p_goes_on[WAVES + kAhead], s_goes_on[WAVES + kAhead];      // rows like the one before them: the same prefix, the same sequence
@@ -138,6 +144,11 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
             if (r.lead >= 0) {
                 atomicAdd(&members[r.lead], 1);
                 shared += r.keys >> 4;
+            }
+            if (long_prompts) {
+                if ((t == 0 || before != seq) && (unsigned)seq < (unsigned)prefix.n_seqs) { run_start[seq] = t; run_pos[seq] = r.pos - r.keys; }
+                if (t > 0 && before != seq && (unsigned)before < (unsigned)prefix.n_seqs) run_end[before] = t;
+                if (t + 1 == prefix.rows && (unsigned)seq < (unsigned)prefix.n_seqs) run_end[seq] = t + 1;
             }
             if (t == 0 || before != seq || (rule.tiles && (r.pos - r.keys) % rule.tg_many == 0)) own += (r.pos - r.keys + 16) >> 4;
         }
@@ -241,7 +252,9 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
             if (live && r.pos >= 0) {
                 const int tg = rule.tg_many, block = quotient(p, tg, rule.many_magic);
                 single = s_at + 1 + s_run.behind <= rule.short_tokens;
-                s_ct = single ? item_positions(rule, batch_own, p + s_run.behind + 1) : rule.tiles ? item_positions(rule, batch_own, (block + 1) * tg) : prefill_chunk_positions((block + 1) * tg);
+                const int reach = (block + 1) * tg, prompt = long_prompts ? run_end[r.seq] - run_start[r.seq] : 0;
+                s_ct = single ? item_positions(rule, batch_own, p + s_run.behind + 1) : rule.tiles ? item_positions(rule, batch_own, reach) :
+                       prompt <= kLongRun ? prefill_chunk_positions(reach) : prefill_run_chunk_positions(reach, tg, rule.n_kv, prompt, run_pos[r.seq] + (prompt + 1) / 2);
                 const int at = single ? s_at : same_seq ? p - block * tg : 0;
                 if (at == 0) {                                                                     // rows of the sequence in this item, or in its aligned block
                     s_tok = single ? 1 + s_run.behind : min(tg - (p - block * tg), 1 + s_run.behind);
