@@ -663,7 +663,7 @@ class SharedAttention:
         _on_gpu(self.device)
         nbytes = lib().dyn_attn_shared_workspace_bytes(C.byref(self.batch))
         if nbytes == 0 and T:
-            raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error())
+            _check(lib().dyn_attn_shared(C.byref(self.batch), None))          # refuses the sizes before it looks at anything else
         if workspace is not None and (workspace.dtype != torch.uint8 or workspace.device != self.device or workspace.numel() < nbytes + 256):
             raise ValueError("workspace: %d bytes on %s" % (nbytes + 256, self.device))
         self._workspace = _Workspace(workspace, nbytes + 256, self.device)
@@ -706,7 +706,8 @@ class PagePool:
         _on_gpu(self.device)
         nbytes = lib().dyn_pages_workspace_bytes(C.byref(self.pool), self.max_requests)
         if nbytes == 0:
-            raise DynError(DYN_ERR_INVALID_ARG, dyn_last_error() or "max_requests = %d" % self.max_requests)
+            _check(lib().dyn_pages_copy(C.byref(self.pool), 0, None, None, None))      # refuses the sizes; no pages, no work
+            raise DynError(DYN_ERR_INVALID_ARG, "max_requests = %d" % self.max_requests)
         self._workspace = _Workspace(None, nbytes + 256, self.device)
         self.pool.workspace = self._workspace.aligned()
         self.pool.workspace_bytes = nbytes
