@@ -25,6 +25,7 @@ dyn_status check_sizes(const dyn_attn_batch *b) {
     const int d = b->head_dim;
     if (d < 8 || d > 2 * dyn::kMaxHalfDim || (d & (d - 1))) return fail(DYN_ERR_UNSUPPORTED, "head_dim must be a power of two in 8..256");
     if (b->page_size > 512) return fail(DYN_ERR_UNSUPPORTED, "page_size > 512");
+    if ((long long)b->n_q_heads * d > 0x7fffffffLL) return fail(DYN_ERR_UNSUPPORTED, "rows of %lld elements", (long long)b->n_q_heads * d);
     if (b->kv_chunk_positions != 0 && (b->kv_chunk_positions < 64 || b->kv_chunk_positions > 65536 || b->kv_chunk_positions % b->page_size))
         return fail(DYN_ERR_INVALID_ARG, "kv_chunk_positions = %d: 0, or a multiple of page_size in 64..65536", b->kv_chunk_positions);
     if (b->n_tokens < 0 || b->n_seqs < 0) return fail(DYN_ERR_INVALID_ARG, "negative n_tokens or n_seqs");
