@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import test_gpu_attn_shared as shared
 from test_gpu_attn_shared import Case, group
 from gpu_util import say
 
@@ -43,3 +44,9 @@ def test_probabilities_are_not_rounded_to_bf16(shape, what):
         assert (err <= bound).all(), (t, (err / bound).max().item())
         worst = max(worst, (err / bound).max().item())
     say("%s %s: worst share of the bound %.2f" % (shape, what, worst))
+
+
+@pytest.mark.parametrize("name,prefixes", [("bf16_ps32", {0: (1, [0, 1, 2, 3])}), ("bf16_max", {0: (1, [0, 2, 3])}), ("bf16_hd64", {1: (2, [1, 2, 3])})])
+def test_layers_on_larger_pages_and_other_heads(name, prefixes):
+    """Against the oracle, under every schedule, as the layers of 16-position pages are."""
+    shared.test_layer_with_shared_prefixes(name, prefixes)
