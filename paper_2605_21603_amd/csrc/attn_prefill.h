@@ -73,6 +73,12 @@ struct SubTiles {
     __device__ __forceinline__ int page_of(int sub) const { return (int)__umulhi((unsigned)sub, magic); }     // exact for sub * per below 2^32
 };
 
+// Of two bf16, at positions `first` and first + 1: the bits without infinities and NaN at `late` or behind it.
+__device__ __forceinline__ uint32_t late_mask(uint32_t x, int first, int late) {
+    return (first >= late && (x & 0x7f80u) == 0x7f80u ? 0xffff0000u : ~0u) & (first + 1 >= late && (x & 0x7f800000u) == 0x7f800000u ? 0x0000ffffu : ~0u);
+}
+__device__ __forceinline__ float odd_or_0(bf16_t x) { return (x & 0x7f80u) == 0x7f80u ? __uint_as_float((uint32_t)x << 16) : 0.f; }
+
 // bf16 numbers that a probability is the sum of in its product with V.  Pages of 16: one, rounded as in the layer's own kernels for these shapes (2^-8 of it).  Larger
 // pages without shared prefixes run in the general form with all 24 bits, so with them a probability is two, to 2^-16 of it: the outputs' error against 64 bits is
 // the general form's to three digits (0.00166 of their norm; one part 0.0023, three 0.00166).  32 q heads, 8 kv heads, pages of 32, one / two / three parts / general form:
@@ -98,8 +104,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                                                               bf16_t *__restrict__ out, int ld_out,
                                                               float *__restrict__ part_o, float *__restrict__ part_ml,
                                                               AttnShape sh, const int32_t *__restrict__ plan, int32_t *__restrict__ counter,
-                                                              const int32_t *__restrict__ ct_of_token, int ld_q = 0, SubTiles page = SubTiles{},
-                                                              int32_t *odd = nullptr, int mark = 0) {
+                                                              const int32_t *__restrict__ ct_of_token, int ld_q = 0, SubTiles page = SubTiles{}) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     int32_t *pid = reinterpret_cast<int32_t *>(lds + kRing * kTile);      // physical pages of the chunk
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -120,7 +125,10 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
     for (;;) {
         __builtin_amdgcn_s_waitcnt(0x0f70);                               // the previous item's stores and trailing tile loads
         __syncthreads();                                                  // everyone has read the previous claim and left the ring
-        if (tid == 0) *claim = atomicAdd(counter, 1);
+        if (tid == 0) {
+            *claim = atomicAdd(counter, 1);
+            if constexpr (PARTS) claim[1] = 0;
+        }
         __syncthreads();
         const int taken = *claim;
         if (taken >= n_items) break;
@@ -160,27 +168,6 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
         // keys its first token attends; columns of dead tokens or heads carry zeros and are never stored
         const int wave_min_keys = wave_tok0 < n_tok ? pos_of_token[t0 + wave_tok0] + 1 : 0;
         __syncthreads();                                                  // pid is visible
-        // PARTS: values behind the block's first token, which some columns must not see: its rows are marked in `odd` if they are not all finite
-        if constexpr (PARTS) {
-            const int late0 = max(pos_of_token[t0] + 1, lp0 * PS), late1 = min(n_keys, (lp0 + n_pg) * PS), per = WIDE_PAGES ? page.per : 1;
-            const int most = late0 < late1 ? ((late1 + PS - 1) / PS - late0 / PS) * 256 : 0;
-#pragma clang loop unroll(disable)
-            for (int i = tid; i < most; i += kWaves * 64) {
-                const int sub = late0 / PS + (i >> 8), slot = WIDE_PAGES ? sub - page.page_of(sub) * per : 0, r = i >> 1 & 127, h = i & 1;
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(v_cache + ((size_t)pid[sub - lp0] * sh.n_kv + g) * (PS * HD) * per + r * PS * per + slot * PS + h * 8);
-                bool found = false;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const int at = sub * PS + h * 8 + 2 * d;
-                    found |= at >= late0 && at < late1 && (x[d] & 0x7f80u) == 0x7f80u;
-                    found |= at + 1 >= late0 && at + 1 < late1 && (x[d] & 0x7f800000u) == 0x7f800000u;
-                }
-                if (found) {
-#pragma clang loop unroll(disable)
-                    for (int j = 0; j < n_tok; ++j) odd[t0 + j] = mark;
-                }
-            }
-        }
 
         // Wave w copies one 4 KB page of every tile: K pages 0..3 (waves 0..3), V pages 0..3 (waves 4..7).
         const int wpage = wave & (kTP - 1);
@@ -245,6 +232,32 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
                 for (int d = 0; d < 4; ++d) x[d] &= (n > 2 * d ? 0x0000ffffu : 0u) | (n > 2 * d + 1 ? 0xffff0000u : 0u);
                 *w = x;
             }
+            wait_lgkmcnt<0>();
+        };
+        // PARTS: of positions behind the block's first token some columns must not see the values.  Infinities and NaN among them are taken out by the wave that
+        // copied the page, and come back behind the tile loop for the columns that see them: for the others they are as any finite value.
+        const int late0 = PARTS ? pos_of_token[t0] + 1 : 0;
+        auto take_out = [&](int tile) {
+            const int first = (lp0 + kTP * tile + wpage) * PS;
+            if (first + PS <= late0 || first >= n_keys) return;
+            unsigned char *pb0 = lds + (tile % kRing) * kTile + kTP * 4096 + wpage * 4096;
+            bool found = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = j * 32 + (lane >> 1), h = (lane & 1) ^ ((r >> 2) & 1);   // V row, half of its positions in this slot
+                u32x4 *w = reinterpret_cast<u32x4 *>(pb0 + j * 1024 + lane * 16);
+                u32x4 x = *w;
+                bool here = false;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const uint32_t keep = late_mask(x[d], first + 8 * h + 2 * d, late0);
+                    x[d] &= keep;
+                    here |= keep != ~0u;
+                }
+                if (here) *w = x;
+                found |= here;
+            }
+            if (found) claim[1] = 1;
             wait_lgkmcnt<0>();
         };
 
@@ -357,6 +370,7 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
             if (late) {                                                   // V of tile ti is in the ring before the next phase reads it
                 wait_vm(4);
                 if (ti == n_tile - 1) clear_stale(ti);
+                if (PARTS && ti < n_tile && (lp0 + kTP * (ti + 1)) * PS > late0) take_out(ti);
             }
             __builtin_amdgcn_s_barrier();
             if (late) issue(ti + 2);
@@ -427,6 +441,21 @@ __device__ __forceinline__ void attn_prefill_items(const bf16_t *__restrict__ qk
             __builtin_amdgcn_s_barrier();
         }
         if (!late) __builtin_amdgcn_s_barrier();                          // the late group's last phase
+        if (PARTS && claim[1]) {
+#pragma clang loop unroll(disable)
+            for (int at = max(late0, lp0 * PS); at < min(n_keys, (lp0 + n_pg) * PS); ++at) {
+                const int sub = at / PS, per = WIDE_PAGES ? page.per : 1, slot = at - (WIDE_PAGES ? page.page_of(sub) * per : sub) * PS;
+                const bf16_t *vp = v_cache + ((size_t)pid[sub - lp0] * sh.n_kv + g) * (PS * HD) * per + 4 * lq * PS * per + slot;
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = odd_or_0(vp[(dt * 16 + r) * PS * per]);
+#pragma unroll
+                        for (int q = 0; q < kSets; ++q) acc[q][dt][r] += at < nk[q] ? x : 0.f;
+                    }
+            }
+        }
 
 #pragma unroll
         for (int q = 0; q < kSets; ++q) {

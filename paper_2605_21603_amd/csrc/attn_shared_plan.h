@@ -19,9 +19,6 @@ struct SharedPlan {
     int32_t *items, *p_blocks, *s_blocks;
     // What the lists take, in us of one CU and kv head: [0] the items, [1] the query blocks.
     float *cost;
-    // Per row: the `mark` of the launch that found infinities or NaN among the values that only later tokens of its sequence see, in what it is served
-    // with (SharedArgs; 0: none did).  A word per row and a mark per layer, so that no row pays for another sequence's, and no layer for an earlier one's.
-    int32_t *odd;
 };
 constexpr int kOwnItem = 1 << 30;
 

@@ -160,7 +160,7 @@ Sizes tensor_sizes(const dyn_layer *L, int T, int max_pages, bool prompts, bool 
         z.max_chunks = std::max(z.max_chunks, dyn::attn_prefill_max_chunks((long)std::max(max_pages, 1) * c.page_size));
     z.prefix_chunks = prefix ? dyn::attn_prefix_max_chunks(c.dtype, sh) : 0;
     if (prefix) z.max_chunks = dyn::attn_own_max_chunks(c.dtype, sh);
-    // per dispatch: two lists of 2 header words + 2 per entry, one chunk size per token; with shared prefixes three lists and seven arrays of a
+    // per dispatch: two lists of 2 header words + 2 per entry, one chunk size per token; with shared prefixes three lists and six arrays of a
     // word per token
     const dyn::AttnPrefix shared{nullptr, nullptr, 0, z.prefix_chunks, nullptr, nullptr, 0};
     const dyn::AttnShape lists{c.n_q_heads, c.n_kv_heads, c.head_dim, c.page_size, max_pages, L->chunk_pages, z.max_chunks, 0};

@@ -28,7 +28,6 @@ struct SharedArgs {
     const int32_t *block_table;
     SharedPlan plan;
     AttnShape sh;                         // rows of a table of one wide row; max_chunks: of both halves
-    int mark;                             // what this launch writes into plan.odd
     int ld_q, shared_slots;               // partials of own keys lie behind shared_slots chunks of shared ones
     float *part_o, *part_ml;
     prefill::SubTiles page;
@@ -42,11 +41,6 @@ struct Item {
     int full;                             // the first position that its first token does not see
     const int32_t *table;
 };
-
-// Whether one of two bf16, at positions `first` and first + 1, lies at `full` or behind it and is an infinity or NaN.
-__device__ __forceinline__ bool late_odd(uint32_t x, int first, int full) {
-    return (first >= full && (x & 0x7f80u) == 0x7f80u) || (first + 1 >= full && (x & 0x7f800000u) == 0x7f800000u);
-}
 
 __device__ __forceinline__ Item fetch_item(const SharedArgs &a, int i) {
     Item m;
@@ -120,6 +114,7 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
     };
     f32x4 acc[8];
     float m_run, l_run;
+    bool odd;                                // of the chunk: infinities or NaN were taken out
     auto multiply = [&](auto buf, const Item &m, int tile) {
         constexpr int B = decltype(buf)::value;
         const int at = (m.first + tile * TILE) * 16;
@@ -146,16 +141,18 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
                     vr[B][i][dt][0] &= (n > 0 ? 0x0000ffffu : 0u) | (n > 1 ? 0xffff0000u : 0u);
                     vr[B][i][dt][1] &= (n > 2 ? 0x0000ffffu : 0u) | (n > 3 ? 0xffff0000u : 0u);
                 }
+                // of a token that only later columns see, infinities and NaN neither: they come back behind the chunk for the columns that see them
                 if (m.full < m.end) {
                     bool found = false;
 #pragma unroll
                     for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) found |= late_odd(vr[B][i][dt][h], at + 16 * i + 4 * lq + 2 * h, m.full);
-                    if (found) {
-#pragma clang loop unroll(disable)
-                        for (int j = 0; j < m.n_tok; ++j) a.plan.odd[m.t + j] = a.mark;
-                    }
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t keep = prefill::late_mask(vr[B][i][dt][h], at + 16 * i + 4 * lq + 2 * h, m.full);
+                            vr[B][i][dt][h] &= keep;
+                            found |= keep != ~0u;
+                        }
+                    odd |= __any(found) != 0;
                 }
             }
         }
@@ -207,6 +204,7 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
         for (int dt = 0; dt < 8; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         m_run = -INFINITY;
         l_run = 0.f;
+        odd = false;
         const int pairs = (cur.last - cur.first + 2 * TILE) / (2 * TILE);     // an odd tile at the end is walked masked
         for (int pr = 0; pr < pairs; ++pr) {
             load(b1, cur, 2 * pr + 1);
@@ -219,6 +217,20 @@ __device__ __forceinline__ void serve_items(const SharedArgs &a, int block, int 
             __builtin_amdgcn_sched_barrier(0);
             multiply(b1, cur, 2 * pr + 1);
             __builtin_amdgcn_sched_barrier(0);
+        }
+        if (odd) {
+#pragma clang loop unroll(disable)
+            for (int at = max(cur.full, cur.first * 16); at < cur.end; ++at) {
+                const int sub = at >> 4, per = WIDE_PAGES ? a.page.per : 1, in = WIDE_PAGES ? a.page.page_of(sub) : sub, ps = 16 * per;
+                const bf16_t *vp = a.v + (((size_t)cur.table[in] * sh.n_kv + cur.g) * HD + 4 * lq) * ps + at - in * ps;
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = prefill::odd_or_0(vp[(dt * 16 + r) * ps]);
+                        acc[dt][r] += at < cur.full + col_tok ? x : 0.f;
+                    }
+            }
         }
         float l = l_run;
         l += __shfl_xor(l, 16, 64);
@@ -259,77 +271,27 @@ __global__ __launch_bounds__(prefill::kWaves * 64, 1) void attn_shared_kernel(Sh
         int32_t *const list = own ? w.s_blocks : w.p_blocks;
         if (list[0] == 0) continue;
         prefill::attn_prefill_items<true, WIDE_PAGES>(a.q, own ? w.s_seq : w.p_seq, own ? w.s_pos : w.p_pos, a.block_table, a.k, a.v, nullptr, 0,
-                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q, a.page, w.odd, a.mark);
+                                          a.part_o + (own ? behind * HD : 0), a.part_ml + (own ? behind * 2 : 0), a.sh, list, list + 1, own ? w.s_ct : w.p_ct, a.ld_q, a.page);
     }
-}
-
-// What the merge needs to attend a row's own keys again.
-struct MendArgs {
-    const bf16_t *q, *k, *v;
-    const int32_t *block_table, *s_seq, *odd;
-    int mark, ld_q;
-};
-
-// Positions first .. end - 1 for one column (q: its 128 values), by a half-wave: a position to a lane for the scores, four head-dim indices for the values, and
-// nothing read behind `end`.
-__device__ __forceinline__ void attend_plain(const MendArgs &a, const bf16_t *q, const int32_t *table, int n_kv, int g, int ps, int first, int end, float *po, float *pml) {
-    const int sub = threadIdx.x & 31;
-    const float scale = 1.4426950408889634f / sqrtf((float)HD);
-    float top = -INFINITY, l = 0.f;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto place = [&](int j, int &slot) {
-        const int at = j / ps;
-        slot = j - at * ps;
-        return (size_t)table[at] * n_kv + g;
-    };
-#pragma clang loop unroll(disable)
-    for (int j0 = first; j0 < end; j0 += 32) {
-        const int n = min(32, end - j0);
-        int slot;
-        const size_t page = place(j0 + min(sub, n - 1), slot);
-        const bf16_t *kp = a.k + (page * ps + slot) * HD;
-        float s = 0.f;
-#pragma clang loop unroll(disable)
-        for (int i = 0; i < HD; ++i) s += bf2f(q[i]) * bf2f(kp[i]);
-        s = sub < n ? s * scale : -INFINITY;
-        float now = fmaxf(top, s);
-        for (int off = 16; off >= 1; off >>= 1) now = fmaxf(now, __shfl_xor(now, off, 32));
-        const float ref = now == -INFINITY ? 0.f : now, alpha = exp2f(top - ref), p = exp2f(s - ref);
-        top = now;
-        l = l * alpha + p;
-        o *= alpha;
-#pragma clang loop unroll(disable)
-        for (int i = 0; i < n; ++i) {
-            const float pi = __shfl(p, i, 32);
-            const bf16_t *vp = a.v + (place(j0 + i, slot) * HD + 4 * sub) * ps + slot;
-            o += pi * f32x4{bf2f(vp[0]), bf2f(vp[ps]), bf2f(vp[2 * ps]), bf2f(vp[3 * ps])};
-        }
-    }
-    for (int off = 16; off >= 1; off >>= 1) l += __shfl_xor(l, off, 32);
-    *reinterpret_cast<f32x4 *>(po + 4 * sub) = o;
-    if (sub == 0) { pml[0] = top; pml[1] = l; }
 }
 
 // Merge of a row's partials, shared chunks first, in order; four head-dim indices to a lane, two sets of them in the WIDE form (head dims above
 // 128).  Where there are rows to fill the chip a half-wave merges a (token, q head); else (SPLIT) a workgroup does, its eight half-waves every
 // eighth chunk each and the eight results in order through LDS.  A row without keys is zero.  What it costs is two dependent loads, of the row's chunk counts and
 // of its partials, so the first of those are all on their way beside the maxima and sums that weigh them.
-// MEND: where the launch before found values that are not finite among those of later tokens than a row's, in what the row was served with, these met its
-// zero probabilities (0 * NaN), so all its own keys are attended again, plainly, in that launch's chunks.  Sequences are whole in a dispatch, so which rows
-// these are does not depend on the schedule.
-template <typename T, bool BASE2, bool WIDE, bool SPLIT, bool MEND>
-__global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_combine_kernel(float *part_o, float *part_ml,
+template <typename T, bool BASE2, bool WIDE, bool SPLIT>
+__global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_combine_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml,
                                                                   const int32_t *__restrict__ p_pos, const int32_t *__restrict__ p_ct,
                                                                   const int32_t *__restrict__ s_pos, const int32_t *__restrict__ s_ct,
                                                                   int shared_slots, T *__restrict__ out, int ld_out, AttnShape sh,
-                                                                  int32_t *__restrict__ counter0, int32_t *__restrict__ counter1, MendArgs mend) {
+                                                                  int32_t *__restrict__ counter0, int32_t *__restrict__ counter1) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     constexpr int SETS = WIDE ? 2 : 1, MOST_LOADS = 8 / SETS, STEP = SPLIT ? 8 : 1;
     // the lists' query blocks have all been claimed: from the start again for the next layer
     if (counter0 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) *(threadIdx.x ? counter1 : counter0) = 0;
     const int t = blockIdx.x, sub = threadIdx.x & 31, half = threadIdx.x >> 5, d = sh.head_dim, h = SPLIT ? (int)blockIdx.y : (int)blockIdx.y * 8 + half;
     if (h >= sh.n_q) return;
-    const int pp = p_pos[t], sp = s_pos[t], pc = p_ct[t], sc = s_ct[t], odd = MEND ? mend.odd[t] : 0;
+    const int pp = p_pos[t], sp = s_pos[t], pc = p_ct[t], sc = s_ct[t];
     const int n_shared = pp < 0 ? 0 : (pp + pc) / pc, n = n_shared + (sp < 0 ? 0 : (sp + sc) / sc);
     const int c0 = SPLIT ? half : 0, count = (n - c0 + STEP - 1) / STEP;                     // chunks c0, c0 + STEP, ...
     f32x4 acc[SETS];
@@ -343,18 +305,6 @@ __global__ __launch_bounds__(256, SPLIT ? 1 : WIDE ? 6 : 8) void attn_shared_com
             const int c = c0 + i * STEP;
             return first + (size_t)(c < n_shared ? c : shared_slots + c - n_shared) * next;
         };
-        if constexpr (MEND) {
-            if (odd == mend.mark) {
-#pragma clang loop unroll(disable)
-                for (int i = 0; i < count; ++i) {
-                    const int c = c0 + i * STEP - n_shared, g = h / (sh.n_q / sh.n_kv);
-                    if (c >= 0)
-                        attend_plain(mend, mend.q + (size_t)t * mend.ld_q + h * HD, mend.block_table + mend.s_seq[t], sh.n_kv, g, sh.page_size, c * sc, min((c + 1) * sc, sp + 1),
-                                     part_o + at(i) * HD, part_ml + at(i) * 2);
-                }
-                __threadfence_block();
-            }
-        }
         auto ml_of = [&](int i) { return i < count ? *reinterpret_cast<const f32x2 *>(part_ml + at(i) * 2) : f32x2{-INFINITY, 0.f}; };
         auto walk = [&](auto loads) {
             constexpr int LOADS = decltype(loads)::value;
@@ -463,7 +413,7 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
             if (e != hipSuccess) return e;
             attr_set[sh.page_size != 16] |= bit;
         }
-        const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, layer + 1, ld_q, prefix.max_chunks, part_o,
+        const SharedArgs a{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w, part, ld_q, prefix.max_chunks, part_o,
                            part_ml, prefill::SubTiles{sh.page_size / 16, (unsigned)((0x100000000ull + sh.page_size / 16 - 1) / (sh.page_size / 16))}};
         const long most = (long)rows * sh.n_kv * part.max_chunks;
         const int cus = sh.n_cus > 0 && sh.n_cus < 256 ? sh.n_cus : 256;
@@ -481,23 +431,19 @@ hipError_t launch_attention_shared(int dtype, const void *q, int ld_q, const int
     // which of the two depends on the batch, so that a row's bits do not depend on the dispatch it is in
     const bool split = (long)prefix.rows * sh.n_q <= 512;
     const dim3 grid(rows, split ? sh.n_q : (sh.n_q + 7) / 8), block(256);
-    const MendArgs mend{(const bf16_t *)q, (const bf16_t *)k_cache, (const bf16_t *)v_cache, block_table, w.s_seq, w.odd, layer + 1, ld_q};
-#define DYN_COMBINE_AS(T, B2, WIDE, SPLIT, MEND)                                                                                                            \
-    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE, SPLIT, MEND>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,        \
-                       prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, lists ? w.s_blocks + 1 : nullptr, mend)
-#define DYN_COMBINE(T, B2)                                                                                                    \
-    do {                                                                                                                      \
-        if (split) {                                                                                                          \
-            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, true, false); else DYN_COMBINE_AS(T, B2, false, true, false);   \
-        } else {                                                                                                              \
-            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, false, false); else DYN_COMBINE_AS(T, B2, false, false, false); \
-        }                                                                                                                     \
+#define DYN_COMBINE_AS(T, B2, WIDE, SPLIT)                                                                                                            \
+    hipLaunchKernelGGL((attn_shared_combine_kernel<T, B2, WIDE, SPLIT>), grid, block, 0, s, part_o, part_ml, w.p_pos, w.p_ct, w.s_pos, w.s_ct,        \
+                       prefix.max_chunks, (T *)out, ld_out, part, lists ? w.p_blocks + 1 : nullptr, lists ? w.s_blocks + 1 : nullptr)
+#define DYN_COMBINE(T, B2)                                                                                     \
+    do {                                                                                                       \
+        if (split) {                                                                                           \
+            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, true); else DYN_COMBINE_AS(T, B2, false, true);   \
+        } else {                                                                                               \
+            if (sh.head_dim > 128) DYN_COMBINE_AS(T, B2, true, false); else DYN_COMBINE_AS(T, B2, false, false); \
+        }                                                                                                      \
     } while (0)
-    if (lists) {
-        if (split) DYN_COMBINE_AS(bf16_t, true, false, true, true);
-        else DYN_COMBINE_AS(bf16_t, true, false, false, true);
-    } else if (dtype == 0) DYN_COMBINE(float, false);
-    else if (form == SHARE_TILES) DYN_COMBINE(bf16_t, true);
+    if (dtype == 0) DYN_COMBINE(float, false);
+    else if (form != SHARE_NOTHING) DYN_COMBINE(bf16_t, true);
     else DYN_COMBINE(bf16_t, false);
 #undef DYN_COMBINE
 #undef DYN_COMBINE_AS

@@ -291,7 +291,6 @@ __global__ __launch_bounds__(WAVES * 64) void attn_shared_plan_kernel(const int3
             w.p_seq[t] = on ? r.lead * max_pages : -1;
             w.p_ct[t] = p_ct;
             w.s_ct[t] = SHARE ? s_ct : rule.most_positions;
-            w.odd[t] = 0;
             if constexpr (SHARE) {
                 int32_t *at = few ? w.items + 2 + 2 * (size_t)start[0] : w.p_blocks + 2 + 2 * (size_t)start[1];
                 for (int c = 0; c < p_n; ++c) { *at++ = t; *at++ = c | (p_tok << 20); }
@@ -346,13 +345,13 @@ int attn_own_max_chunks(int dtype, const AttnShape &sh) {
 
 size_t attn_shared_plan_words(const AttnShape &sh, const AttnPrefix &prefix, int rows) {
     const size_t own = (size_t)sh.max_chunks * rows, shared = (size_t)prefix.max_chunks * rows;
-    return (size_t)rows * 7 + 8 + 4 * (own + shared);          // (for rows together no more than for each of them alone)
+    return (size_t)rows * 6 + 8 + 4 * (own + shared);          // (for rows together no more than for each of them alone)
 }
 
 SharedPlan attn_shared_plan(int32_t *plan, const AttnShape &sh, const AttnPrefix &prefix, int rows) {
     SharedPlan w;
     int32_t *at = plan;
-    for (int32_t **a : {&w.p_seq, &w.p_pos, &w.p_ct, &w.s_seq, &w.s_pos, &w.s_ct, &w.odd}) { *a = at; at += rows; }
+    for (int32_t **a : {&w.p_seq, &w.p_pos, &w.p_ct, &w.s_seq, &w.s_pos, &w.s_ct}) { *a = at; at += rows; }
     const size_t own = (size_t)sh.max_chunks * rows, shared = (size_t)prefix.max_chunks * rows;
     w.cost = (float *)at;
     w.items = at + 2;

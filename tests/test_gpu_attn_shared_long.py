@@ -29,13 +29,13 @@ def run_rule(reach, tg, n_kv, rows, mean):
 
 def chunks_of_own_keys(att):
     """The chunk length of every row's own keys, from the plan that the call left in its workspace: partials (o, then m and l) of C chunks a token, then
-    seven arrays of a word per row - the sixth of them this - and the lists."""
+    six arrays of a word per row - the sixth of them this - and the lists."""
     T, n_q, hd = att.out.shape
     up = lambda n: (n + 255) & ~255
     parts = lambda c: up(T * c * n_q * hd * 4) + up(T * c * n_q * 2 * 4)
-    c = next(c for c in range(1, 500) if parts(c) + up((7 * T + 8 + 4 * c * T) * 4) == att.batch.workspace_bytes)
+    c = next(c for c in range(1, 500) if parts(c) + up((6 * T + 8 + 4 * c * T) * 4) == att.batch.workspace_bytes)
     at = att.batch.workspace - att.workspace.data_ptr() + parts(c)
-    return att.workspace[at:at + 7 * T * 4].view(torch.int32).view(7, T)[5].cpu().numpy()
+    return att.workspace[at:at + 6 * T * 4].view(torch.int32).view(6, T)[5].cpu().numpy()
 
 
 def test_prompts_of_more_and_of_fewer_rows(monkeypatch):
