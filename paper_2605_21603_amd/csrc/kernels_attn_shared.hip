@@ -7,9 +7,11 @@
 // them an attention of every sequence for itself, as a decode's or a prompt's that starts at P.  Three launches: the plan
 // (kernels_attn_shared_plan.hip), the keys (attn_shared_kernel, or attn_tile of kernels_attn_generic.hip for what it does not
 // take), and the merge of a row's chunks.
-// 32 q heads, 8 kv heads, 128 wide, caches out of reach of the last call, plan + keys + merge: 5 tokens behind 512 positions 5.4 + 6.8 + 4.2 us; 64 behind 2048 with
-// 16 to 1024 of their own, 162 MB, 6.0 + 49 + 5.4; 256 on 4 prefixes, 1.19 GB, 6.8 + 250 (4.7 TB/s) + 9.6; 12 prompts of 33 to 300 tokens behind 4096 positions, 1.08e11
-// operations, 13 + 150 (0.72 PFLOP/s) + 14.
+// 32 q heads, 8 kv heads, 128 wide, caches out of reach of the last call, plan + keys + merge: 5 tokens behind 512 positions 5.2 + 7.3 + 4.0 us; 64 behind 2048 with
+// 16 to 1024 of their own, 162 MB, 5.9 + 49 + 5.2; 256 on 4 prefixes, 1.19 GB, 6.6 + 252 (4.7 TB/s) + 9.5; 12 prompts of 33 to 300 tokens behind 4096 positions, 1.08e11
+// operations, 13 + 132 (0.82 PFLOP/s) + 14.
+// A token's product has columns of tokens that do not see it, where its probability is zero: infinities and NaN among its values are taken out of the product
+// and put back for the columns that see them, so that for the others it is as any finite value (64 sequences of 4 tokens, one of them with NaN: 65.6 -> 66.8 us).
 #include <algorithm>
 #include <atomic>
 

@@ -5,7 +5,7 @@
 // sequence, the last key for the position), and work lists name what exists of it.  Who shares with a row, and how long chunks are, is counted
 // over the whole batch and not over the dispatch, so a row's sums do not depend on the schedule.  A row that stands inside the shared positions, alone with its lead or outside the table attends all its keys as its own.
 // What it costs is the latency of its loads, so everything that is looked at twice is kept in LDS: leads and pages of all sequences, and
-// which rows go on with the row before them.  5 rows 5.4 us, 256 rows of 256 sequences 6.8, 1563 of 12 sequences 13, 5387 of 242 sequences 32 (a round of 1024 rows 4.5).
+// which rows go on with the row before them.  5 rows 5.2 us, 256 rows of 256 sequences 6.6, 1563 of 12 sequences 13, 5387 of 242 sequences 29 (a round of 1024 rows 4).
 #include <algorithm>
 
 #include "attn_shared_plan.h"
