@@ -596,11 +596,16 @@ class _Workspace:
 
 
 def _empty_on(stream: Optional[torch.cuda.Stream], n: int, device) -> torch.Tensor:
-    """An int32 result that a kernel on `stream` writes: its memory is that stream's, which no other tensor has before or behind it in another order."""
+    """An int32 result that a kernel on `stream` writes: its memory is that stream's, which no other tensor has before or behind it in another order, and stays the
+    result's while the current stream, where the caller reads it, is not through with what was queued when it is dropped."""
     if stream is None:
         return torch.empty(n, dtype=torch.int32, device=device)
+    reader = torch.cuda.current_stream(device)
     with torch.cuda.stream(stream):
-        return torch.empty(n, dtype=torch.int32, device=device)
+        t = torch.empty(n, dtype=torch.int32, device=device)
+    if reader != stream:
+        t.record_stream(reader)
+    return t
 
 
 _current_device = torch._C._cuda_getDevice

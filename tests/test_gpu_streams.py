@@ -41,12 +41,31 @@ def test_results_belong_to_the_calls_stream(what):
     assert [r.tolist() for r in results] == want
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
-        torch.cuda._sleep(100_000_000)                  # the call lies behind this
+        torch.cuda._sleep(800_000_000)                  # the call lies behind this
     ptrs = [(r.data_ptr(), r.numel() * 4) for r in results_of(other, what, s)]
     assert not s.query()
     for ptr, nbytes in ptrs:
         assert not taken_again(ptr, nbytes)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("what", ["resize", "fork", "compact"])
+def test_results_that_the_current_stream_still_reads(what):
+    """Dropped before the current stream has come to the copy of it: the call's stream does not get the memory back until then."""
+    pool, s = page_pool(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    results = results_of(pool, what, s)
+    s.synchronize()
+    want = [(r + 0).tolist() for r in results]          # (the kernel is loaded)
+    torch.cuda._sleep(800_000_000)
+    read = [r + 0 for r in results]
+    ptrs = [(r.data_ptr(), r.numel() * 4) for r in results]
+    del results
+    assert not torch.cuda.current_stream().query()
+    with torch.cuda.stream(s):
+        assert not any(taken_again(*p) for p in ptrs)
+    torch.cuda.synchronize()
+    assert [r.tolist() for r in read] == want
 
 
 def test_arrays_of_a_call_are_kept_until_it_has_read_them():
@@ -55,7 +74,7 @@ def test_arrays_of_a_call_are_kept_until_it_has_read_them():
     rows, lengths = ints([2, 3, 6]), ints([33, 160, 1])
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
-        torch.cuda._sleep(100_000_000)
+        torch.cuda._sleep(800_000_000)
     status = pool.resize(rows, lengths, stream=s)
     ptrs = [rows.data_ptr(), lengths.data_ptr()]
     del rows, lengths
@@ -79,7 +98,7 @@ def test_a_handle_dropped_while_its_call_waits(make, use, current):
     handle, s = make(), torch.cuda.Stream()
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
-        torch.cuda._sleep(100_000_000)
+        torch.cuda._sleep(800_000_000)
         if current:
             use(handle, None)
     if not current:
